@@ -63,6 +63,7 @@ extern "C" {
 #define ENTRO_MAX_CHUNK_SYMBOLS 16384
 #define ENTRO_STATIC_MAX_TENSORS 8
 #define ENTRO_GEMV_MAX_BATCH 8
+#define ENTRO_KV_ZERO_POINT 128
 
 typedef enum {
     ENTRO_OK = 0,
@@ -73,7 +74,8 @@ typedef enum {
     ENTRO_ERR_CORRUPT_STREAM = 5,  /* stream, index and codebook do not agree */
     ENTRO_ERR_CUDA = 6,            /* a CUDA runtime call failed */
     ENTRO_ERR_UNSUPPORTED = 7,
-    ENTRO_ERR_TOO_MANY_TENSORS = 8 /* more tensors than entro_decode_dequant_static has room for */
+    ENTRO_ERR_TOO_MANY_TENSORS = 8, /* more tensors than entro_decode_dequant_static has room for */
+    ENTRO_ERR_NO_PAGES = 9         /* a key/value cache has no page left, or a table row is full */
 } entro_status;
 
 /* Every tensor is quantised in one of two modes, unsigned or asymmetric, chosen from its
@@ -401,6 +403,142 @@ entro_status entro_gemv_fp16(const void *w_fp16_dev, uint32_t rows, uint32_t col
  */
 entro_status entro_decode_dequant_static(const entro_tensor_desc *descs_host, int ntensors,
                                          uint32_t *status_dev, void *cuda_stream);
+
+/*
+ * The key/value cache of one layer, held in 8 bits, and attention over it: the other memory a
+ * token-generation step reads beside the compressed weights.  Values have the weights' form,
+ * w_hat = s * (u - z), with z = ENTRO_KV_ZERO_POINT and one scale s per page, key / value and head.
+ *
+ *  - A page holds page_tokens consecutive tokens of one sequence, keys and values of all heads:
+ *    codes [2][kv_heads][page_tokens][head_dim] (0 = keys, 1 = values), scales [2][kv_heads].
+ *  - A sequence is a slot: a row of the table (the page of each of its blocks of page_tokens
+ *    tokens, -1 for none) and a length in tokens.  Entries behind the length are -1.
+ *  - refs counts the table entries that name a page; 0 = the page is free.  entro_kv_fork lets
+ *    sequences share pages; a page that is not full belongs to one sequence only.
+ *  - page_tokens is 16, 32, 64 or 128; head_dim 64, 96 or 128 (ENTRO_ERR_UNSUPPORTED otherwise).
+ *  - codes 16-byte aligned, the other arrays 4-byte, work_dev 16-byte.  The arrays are the
+ *    caller's; work_dev has entro_kv_work_bytes(cache) bytes, all zero before the first use, and
+ *    may be shared by caches whose calls do not overlap on the GPU.  Calls on one cache must not
+ *    overlap either (one stream, or ordered with events).
+ *  - Lengths, tables and counts live on the device and are read there: the calls below synchronise
+ *    nothing, and a step (reserve, append, attention) can be captured in a CUDA graph.
+ *  - Page numbers outside the pool and slots outside the table are never followed: such tokens
+ *    count as absent.  What went wrong on the device is kept in work_dev for entro_kv_status.
+ */
+typedef enum { ENTRO_FLOAT16 = 0, ENTRO_BFLOAT16 = 1 } entro_float_type;
+
+typedef struct {
+    uint8_t *codes_dev;      /* [pages][2][kv_heads][page_tokens][head_dim] */
+    float *scales_dev;       /* [pages][2][kv_heads] */
+    int32_t *table_dev;      /* [slots][table_width] */
+    int32_t *lens_dev;       /* [slots] */
+    int32_t *refs_dev;       /* [pages] */
+    void *work_dev;
+    uint64_t work_bytes;
+    uint32_t pages, kv_heads, page_tokens, head_dim, slots, table_width;
+} entro_kv_cache;
+
+/* The sequences of a call and their rows.  The rows of a sequence are its LAST tokens: a
+ * sequence of length len with r rows brings the tokens at positions len - r .. len - 1 (rows
+ * whose position would be negative are ignored).  Every slot at most once. */
+typedef struct {
+    uint32_t n;                    /* sequences */
+    uint32_t rows;                 /* rows of all sequences together */
+    const int32_t *slots_dev;      /* [n], NULL: slot i is sequence i */
+    const int32_t *row_start_dev;  /* [n + 1] ascending, first row of each sequence, row_start[n] = rows;
+                                      NULL: one row each (rows = n) */
+} entro_kv_batch;
+
+/* Keys and values of rows outside the cache: element (row, head, d) at
+ * base[row * row_stride + head * head_stride + d]; bases 16-byte aligned, strides in elements
+ * and multiples of 8 (a slice of a fused projection is fine). */
+typedef struct {
+    void *k_dev, *v_dev;
+    int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+    int32_t type;                  /* entro_float_type */
+    int32_t reserved;              /* 0 */
+} entro_kv_rows;
+
+typedef struct {
+    const void *q_dev;             /* [rows][q_heads][head_dim], strides as for entro_kv_rows */
+    void *out_dev;                 /* the same shape and type, strides of its own; must not overlap q */
+    float *lse_dev;                /* [rows][q_heads] natural log of the softmax sum, or NULL */
+    int64_t q_row_stride, q_head_stride, out_row_stride, out_head_stride;
+    uint32_t q_heads;              /* a multiple of kv_heads; query head h reads kv head h / (q_heads / kv_heads) */
+    uint32_t max_rows;             /* no sequence of the batch has more rows (0: not known) */
+    uint32_t window;               /* 0: none */
+    uint32_t sinks;
+    float softmax_scale;           /* 0: 1 / sqrt(head_dim) */
+    int32_t type;                  /* entro_float_type of q and out */
+} entro_kv_query;
+
+/* Bytes of work_dev for this cache (only its sizes are read); 0 on a bad argument. */
+uint64_t entro_kv_work_bytes(const entro_kv_cache *cache);
+
+/*
+ * Make room for the batch's rows: every sequence grows by its number of rows and gets the pages
+ * it needs for them, the lowest free ones, sequence after sequence in the batch's order.  If the
+ * pool or a table row is too small, the pages that are there are handed out in the same order,
+ * entries left over stay -1, the length grows all the same (nothing that is appended can then
+ * land on another token; what has no page is dropped), and entro_kv_status reports
+ * ENTRO_ERR_NO_PAGES.  Asynchronous.
+ */
+entro_status entro_kv_reserve(const entro_kv_cache *cache, const entro_kv_batch *batch, void *cuda_stream);
+
+/*
+ * Quantise the rows and write them to their places (reserved before).  In every page that gets
+ * a row, for each head, keys and values apart, in IEEE fp32:
+ *   s = max(s_old, max |x| of the page's new rows / 127, 2^-60), s_old = 0 if the page's first
+ *   token is among the new rows;  u = clamp(rne(x / s), -127, 127) + z.
+ * Tokens that were in the page keep their value as nearly as the new scale allows:
+ * u' = rne((u - z) * (s_old / s)) + z, unchanged where s = s_old.  A NaN is stored as 0, an
+ * infinity as the end of the range, the maximum is over the finite values, and entro_kv_status
+ * reports ENTRO_ERR_NONFINITE.  Asynchronous.
+ */
+entro_status entro_kv_append(const entro_kv_cache *cache, const entro_kv_batch *batch, const entro_kv_rows *rows,
+                             void *cuda_stream);
+
+/* The rows as the cache holds them: rne(s * (u - z)) in the type of `rows`; rows without a token
+ * or a page are 0.  Asynchronous. */
+entro_status entro_kv_read(const entro_kv_cache *cache, const entro_kv_batch *batch, const entro_kv_rows *rows,
+                           void *cuda_stream);
+
+/*
+ * Attention of the rows over their sequences: row at position p sees position j iff j <= p and
+ * (window == 0 or j > p - window or j < sinks); out = sum_j softmax_j(softmax_scale * q . k_j) v_j.
+ * Scores, maxima, sums and the output sum are fp32; the probabilities enter the second product as
+ * fp16, relative to the row's largest (probability times value scale), q and the codes exactly
+ * (q of type bf16 is brought to fp16 by a power of two per row).  A row that sees nothing gets
+ * out = 0 and lse = -infinity.  softmax_scale must be finite and not negative.  Asynchronous.
+ */
+entro_status entro_kv_attention(const entro_kv_cache *cache, const entro_kv_batch *batch, const entro_kv_query *query,
+                                void *cuda_stream);
+
+/*
+ * Page operations.  Planned on the device, asynchronous.
+ * entro_kv_fork: for every i < n, slot dst[i] becomes a copy of slot src[i] as it was before the
+ *   call; what dst[i] held is released.  Full pages are shared, the page that is not full is
+ *   copied into a page of its own (the lowest free ones, in the order of i; taken after the
+ *   releases, but never one that a src of this call ends with).  src[i] == dst[i] does nothing.
+ *   dst must be distinct; src may repeat and may be a dst of another pair.  Without a page for the
+ *   copy the entry is -1 and entro_kv_status reports ENTRO_ERR_NO_PAGES.
+ * entro_kv_free: releases the slots' pages; their lengths become 0.  Slots must be distinct.
+ * entro_kv_trim: releases the pages of the slots that no row at the last position or a later one
+ *   sees with this window and these sinks (their entries become -1; window 0: none).
+ * entro_kv_compact: the live pages behind the first L places (L = number of live pages) move, in
+ *   ascending order, to the free places among the first L; tables follow.  Afterwards pages
+ *   L .. pages - 1 are free.
+ */
+entro_status entro_kv_fork(const entro_kv_cache *cache, const int32_t *src_dev, const int32_t *dst_dev, uint32_t n,
+                           void *cuda_stream);
+entro_status entro_kv_free(const entro_kv_cache *cache, const int32_t *slots_dev, uint32_t n, void *cuda_stream);
+entro_status entro_kv_trim(const entro_kv_cache *cache, const int32_t *slots_dev, uint32_t n, uint32_t window,
+                           uint32_t sinks, void *cuda_stream);
+entro_status entro_kv_compact(const entro_kv_cache *cache, void *cuda_stream);
+
+/* Synchronise cuda_stream, then report and clear what the calls on this cache's work_dev found:
+ * ENTRO_OK, ENTRO_ERR_NO_PAGES, or ENTRO_ERR_NONFINITE (ENTRO_ERR_CUDA if the stream failed). */
+entro_status entro_kv_status(const entro_kv_cache *cache, void *cuda_stream);
 
 /*
  * Synchronise cuda_stream, then report and clear what decode kernels found since the last

@@ -26,7 +26,7 @@ MAX_CHUNK_SYMBOLS = 16384
 MODE_AUTO, MODE_UNSIGNED, MODE_ASYMMETRIC = 0, 1, 2
 
 OK, ERR_INVALID_ARG, ERR_BUFFER_TOO_SMALL, ERR_NONFINITE, ERR_CODE_TOO_LONG, ERR_CORRUPT_STREAM, ERR_CUDA, \
-    ERR_UNSUPPORTED, ERR_TOO_MANY_TENSORS = range(9)
+    ERR_UNSUPPORTED, ERR_TOO_MANY_TENSORS, ERR_NO_PAGES = range(10)
 STATIC_MAX_TENSORS = 8
 GEMV_MAX_BATCH = 8
 DEFAULT_DECODE_CONFIG = (12, 32, 1, 1792)   # lut_bits, warps_per_cta, ctas_per_sm, chunks_per_item
@@ -95,6 +95,20 @@ class HostIO(C.Structure):
 _lib = None
 
 
+def _bind_kv(L) -> None:
+    # the key/value calls take the addresses of argument blocks that kv_cache.py packs
+    vp, u32 = C.c_void_p, C.c_uint32
+    L.entro_kv_work_bytes.restype = C.c_uint64
+    L.entro_kv_work_bytes.argtypes = [vp]
+    L.entro_kv_reserve.argtypes = [vp, vp, vp]
+    L.entro_kv_append.argtypes = L.entro_kv_read.argtypes = L.entro_kv_attention.argtypes = [vp, vp, vp, vp]
+    L.entro_kv_fork.argtypes = [vp, vp, vp, u32, vp]
+    L.entro_kv_free.argtypes = [vp, vp, u32, vp]
+    L.entro_kv_trim.argtypes = [vp, vp, u32, u32, u32, vp]
+    L.entro_kv_compact.argtypes = [vp, vp]
+    L.entro_kv_status.argtypes = [vp, vp]
+
+
 def lib():
     """The loaded library.  Raises if it has not been built (python -m paper_2505_02380_b200.build)."""
     global _lib
@@ -140,6 +154,7 @@ def lib():
         L.entro_check_violations.argtypes = []
         L.entro_kernel_launch_count.restype = u64
         L.entro_kernel_launch_count.argtypes = []
+        _bind_kv(L)
         L.entro_status_string.restype = C.c_char_p
         L.entro_status_string.argtypes = [i32]
         for name in EXPORTS:
@@ -155,7 +170,8 @@ EXPORTS = ["entro_quantize_tensor", "entro_quantize_blocks", "entro_histogram", 
            "entro_decode_dequant_batched", "entro_decode_dequant_batched_host", "entro_decode_dequant_static",
            "entro_decode_dequant_gemv", "entro_gemv_prepare", "entro_gemv_run", "entro_gemv_release", "entro_gemv_fp16", "entro_decode_symbols_batched", "entro_last_device_status",
            "entro_set_decode_config", "entro_checked_build", "entro_check_violations", "entro_profile_begin", "entro_profile_read", "entro_kernel_launch_count",
-           "entro_status_string"]
+           "entro_status_string", "entro_kv_work_bytes", "entro_kv_reserve", "entro_kv_append", "entro_kv_read",
+           "entro_kv_attention", "entro_kv_fork", "entro_kv_free", "entro_kv_trim", "entro_kv_compact", "entro_kv_status"]
 
 
 def status_string(status: int) -> str:
@@ -552,3 +568,8 @@ def entro_check_violations() -> int:
 
 def entro_kernel_launch_count() -> int:
     return int(lib().entro_kernel_launch_count())
+
+
+from .kv_cache import (KV_ZERO_POINT, KvCache, entro_kv_append, entro_kv_attention, entro_kv_compact,  # noqa: E402,F401
+                       entro_kv_create, entro_kv_fork, entro_kv_free, entro_kv_read, entro_kv_reserve, entro_kv_status,
+                       entro_kv_trim)

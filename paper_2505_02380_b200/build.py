@@ -10,7 +10,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libentro.so")
 LIB_CHECKED = os.path.join(HERE, "libentro_checked.so")
-SOURCES = ["entro_runtime.cu", "entro_codebook.cu", "entro_quant.cu", "entro_encode.cu", "entro_decode.cu"]
+SOURCES = ["entro_runtime.cu", "entro_codebook.cu", "entro_quant.cu", "entro_encode.cu", "entro_decode.cu",
+           "entro_kv_store.cu", "entro_kv_pages.cu", "entro_kv_attention.cu"]
 
 
 def _stale(lib: str) -> bool:
@@ -30,7 +31,7 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     if not force and not _stale(LIB):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--threads", "0",
            "--shared", "-Xcompiler", "-fPIC,-ffp-contract=off",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", LIB]
     if checked:

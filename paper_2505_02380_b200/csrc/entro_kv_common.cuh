@@ -1,0 +1,148 @@
+// What the kernels on the paged 8-bit key/value cache share: the cache as a kernel sees it, the
+// places in its work area, argument checks, and small device helpers.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "entro_internal.h"
+
+namespace entro {
+
+constexpr uint32_t kKvStatNoPages = 1u, kKvStatNonfinite = 2u, kKvStatInternal = 4u;
+
+// Work area: a header of counters, then one region that every call uses for itself.
+struct KvWorkHeader {
+    uint32_t status;
+    uint32_t pairs;                 // page copies planned by fork / compact
+    uint32_t pad[30];
+    uint32_t part[128];             // per-CTA counts of the planning cluster
+    uint32_t arrived[1024];         // attention: partial results of a split unit that are in place (zero between calls)
+};
+constexpr uint64_t kKvWorkRegion = (sizeof(KvWorkHeader) + 255) / 256 * 256;
+
+struct Kv {
+    uint8_t* codes;
+    float* scales;
+    int32_t* table;
+    int32_t* lens;
+    int32_t* refs;
+    KvWorkHeader* head;
+    unsigned char* region;
+    uint32_t pages, heads, page_shift, dim, slots, width;
+    __host__ __device__ uint32_t page() const { return 1u << page_shift; }
+    __host__ __device__ uint64_t head_bytes() const { return (uint64_t)dim << page_shift; }
+    __host__ __device__ uint64_t page_bytes() const { return 2ull * heads * head_bytes(); }
+};
+
+struct KvBatch {
+    const int32_t* slots;
+    const int32_t* row_start;
+    uint32_t n, rows;
+    // slot of sequence b, or -1
+    __device__ __forceinline__ int slot(uint32_t b, uint32_t nslots) const
+    {
+        const int s = slots ? __ldg(slots + b) : (int)b;
+        return (uint32_t)s < nslots ? s : -1;
+    }
+    // first row of sequence b and number of its rows, never outside [0, rows]
+    __device__ __forceinline__ int first(uint32_t b) const
+    {
+        return row_start ? min(max(__ldg(row_start + b), 0), (int)rows) : (int)b;
+    }
+    __device__ __forceinline__ int count(uint32_t b) const
+    {
+        return row_start ? max(0, min(__ldg(row_start + b + 1), (int)rows) - first(b)) : 1;
+    }
+};
+
+inline entro_status kv_check(const entro_kv_cache* c, Kv* kv)
+{
+    if (!c || !c->codes_dev || !c->scales_dev || !c->table_dev || !c->lens_dev || !c->refs_dev || !c->work_dev)
+        return ENTRO_ERR_INVALID_ARG;
+    if (!aligned(c->codes_dev, 16) || !aligned(c->work_dev, 16) || !aligned(c->scales_dev, 4) || !aligned(c->table_dev, 4) ||
+        !aligned(c->lens_dev, 4) || !aligned(c->refs_dev, 4))
+        return ENTRO_ERR_INVALID_ARG;
+    const uint64_t need = entro_kv_work_bytes(c);
+    if (need == 0)
+        return c->pages && c->kv_heads && c->slots && c->table_width && c->pages < 0x7fffffffu ? ENTRO_ERR_UNSUPPORTED
+                                                                                                : ENTRO_ERR_INVALID_ARG;
+    if (c->work_bytes < need) return ENTRO_ERR_BUFFER_TOO_SMALL;
+    kv->codes = c->codes_dev;
+    kv->scales = c->scales_dev;
+    kv->table = c->table_dev;
+    kv->lens = c->lens_dev;
+    kv->refs = c->refs_dev;
+    kv->head = (KvWorkHeader*)c->work_dev;
+    kv->region = (unsigned char*)c->work_dev + kKvWorkRegion;
+    kv->pages = c->pages;
+    kv->heads = c->kv_heads;
+    kv->page_shift = c->page_tokens == 16 ? 4 : c->page_tokens == 32 ? 5 : c->page_tokens == 64 ? 6 : 7;
+    kv->dim = c->head_dim;
+    kv->slots = c->slots;
+    kv->width = c->table_width;
+    return ENTRO_OK;
+}
+
+// Checks a batch; *live is false where there is nothing to do.
+inline entro_status kv_check(const entro_kv_cache* c, const entro_kv_batch* b, KvBatch* out)
+{
+    if (!b || !aligned(b->slots_dev, 4) || !aligned(b->row_start_dev, 4)) return ENTRO_ERR_INVALID_ARG;
+    if (b->n > c->slots || b->rows > 0x7fffffffu || (!b->row_start_dev && b->rows != b->n)) return ENTRO_ERR_INVALID_ARG;
+    *out = KvBatch{b->slots_dev, b->row_start_dev, b->n, b->rows};
+    return ENTRO_OK;
+}
+
+inline bool kv_strides_ok(int64_t row, int64_t head) { return row % 8 == 0 && head % 8 == 0; }
+
+namespace {
+
+// Page of block `block` of a slot, or -1.
+__device__ __forceinline__ int kv_page(const Kv& kv, int slot, uint32_t block)
+{
+    if (block >= kv.width) return -1;
+    const int p = __ldg(kv.table + (uint64_t)slot * kv.width + block);
+    return (uint32_t)p < kv.pages ? p : -1;
+}
+
+template <typename T>
+__device__ __forceinline__ float2 to_float2(uint32_t two);
+template <>
+__device__ __forceinline__ float2 to_float2<__half>(uint32_t two) { return __half22float2(*reinterpret_cast<__half2*>(&two)); }
+template <>
+__device__ __forceinline__ float2 to_float2<__nv_bfloat16>(uint32_t two)
+{
+    return make_float2(__uint_as_float(two << 16), __uint_as_float(two & 0xffff0000u));
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t from_float2(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t from_float2<__half>(float a, float b)
+{
+    __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&h);
+}
+template <>
+__device__ __forceinline__ uint32_t from_float2<__nv_bfloat16>(float a, float b)
+{
+    __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&h);
+}
+
+// Largest b with at(b) <= key (at ascending), -1 if there is none; all threads of the block call it and get b.
+template <typename F>
+__device__ __forceinline__ int block_find(uint32_t n, uint32_t key, F at)
+{
+    int found = 0;
+    for (uint32_t base = 0; base < n; base += blockDim.x) {
+        const uint32_t b = base + threadIdx.x;
+        const int here = __syncthreads_count(b < n && at(b) <= key);
+        found += here;
+        if (here < (int)blockDim.x) break;
+    }
+    return found - 1;
+}
+
+}  // namespace
+}  // namespace entro

@@ -1,0 +1,482 @@
+// Page operations of the key/value cache: reserve, fork, free, trim, compact.
+//
+// Each is planned by ONE cluster of eight CTAs (8192 threads): the work is counters and small
+// tables, bound by latency, and a cluster has a hardware barrier and a shared view of memory, so
+// all phases fit in one launch with no host in between.  What has to be copied (fork: the pages
+// that are not full; compact: the pages that move) is left as a list of pairs in the work area for
+// copy_pages_kernel, which spreads it over the whole GPU.
+#include "entro_kv_common.cuh"
+
+namespace entro {
+namespace {
+
+constexpr uint32_t kPlanCtas = 8, kPlanThreads = 1024;
+
+__device__ __forceinline__ void cluster_barrier()
+{
+    // release / acquire at cluster scope: what the CTAs wrote to global memory before is visible after
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ uint32_t plan_rank() { return blockIdx.x * kPlanThreads + threadIdx.x; }
+
+// Sum over the block before this thread; *total gets the block's sum.  All threads call it.
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* total)
+{
+    __shared__ uint32_t warp_sum[32];
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    uint32_t x = v;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, x, s);
+        if (lane >= (uint32_t)s) x += y;
+    }
+    __syncthreads();            // warp_sum of an earlier call has been read
+    if (lane == 31u) warp_sum[warp] = x;
+    __syncthreads();
+    uint32_t w = warp_sum[lane];
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, w, s);
+        if (lane >= (uint32_t)s) w += y;
+    }
+    *total = __shfl_sync(0xffffffffu, w, 31);
+    const uint32_t before = __shfl_sync(0xffffffffu, w, (int)(warp ? warp - 1u : 0u));
+    return x - v + (warp ? before : 0u);
+}
+
+// Pages [lo, hi) of this CTA of the planning cluster.
+__device__ __forceinline__ void segment(uint32_t pages, uint32_t* lo, uint32_t* hi)
+{
+    const uint32_t each = (pages + kPlanCtas - 1u) / kPlanCtas;
+    *lo = min(pages, blockIdx.x * each);
+    *hi = min(pages, *lo + each);
+}
+
+// Number of pages of this CTA's segment that `is` holds for.
+template <typename F>
+__device__ __forceinline__ uint32_t count_pages(uint32_t lo, uint32_t hi, F is)
+{
+    uint32_t n = 0, total;
+    for (uint32_t p = lo + threadIdx.x; p < hi; p += kPlanThreads) n += is(p);
+    block_scan(n, &total);
+    return total;
+}
+
+// Calls put(rank, page) for every page of the segment that `is` holds for, ranks from `rank` on in ascending page order.
+template <typename F, typename P>
+__device__ __forceinline__ void rank_pages(uint32_t lo, uint32_t hi, uint32_t rank, uint32_t want, F is, P put)
+{
+    for (uint32_t base = lo; base < hi && rank < want; base += kPlanThreads) {
+        const uint32_t p = base + threadIdx.x;
+        const uint32_t mine = p < hi && is(p);
+        uint32_t total;
+        const uint32_t at = rank + block_scan(mine, &total);
+        if (mine && at < want) put(at, p);
+        rank += total;
+    }
+}
+
+// part[offset .. + kPlanCtas) holds one count per CTA: the sum before this CTA and the sum of all.
+__device__ __forceinline__ void part_sums(const uint32_t* part, uint32_t* before, uint32_t* all)
+{
+    *before = *all = 0;
+#pragma unroll
+    for (uint32_t c = 0; c < kPlanCtas; ++c) {
+        const uint32_t v = __ldcg(part + c);
+        *before += c < blockIdx.x ? v : 0u;
+        *all += v;
+    }
+}
+
+// The `want` lowest free pages in ascending order into fresh[]; returns how many there are.  The
+// caller has a cluster barrier before (counts final) and one after (fresh[] and refs in place).
+__device__ __forceinline__ uint32_t take_lowest_free(const Kv& kv, uint32_t want, int32_t* fresh, uint32_t* part)
+{
+    uint32_t lo, hi, before, all;
+    segment(kv.pages, &lo, &hi);
+    auto is_free = [&](uint32_t p) { return __ldcg(kv.refs + p) <= 0; };
+    const uint32_t mine = count_pages(lo, hi, is_free);
+    if (threadIdx.x == 0) part[blockIdx.x] = mine;
+    cluster_barrier();
+    part_sums(part, &before, &all);
+    rank_pages(lo, hi, before, want, is_free, [&](uint32_t rank, uint32_t p) {
+        fresh[rank] = (int32_t)p;
+        kv.refs[p] = 1;
+    });
+    return min(all, want);
+}
+
+__device__ __forceinline__ uint32_t blocks_of(const Kv& kv, int len)
+{
+    return len > 0 ? min(kv.width, ((uint32_t)len + kv.page() - 1u) >> kv.page_shift) : 0u;
+}
+
+// ---------------------------------------------------------------------------------- reserve
+
+__global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Kv kv, KvBatch batch)
+{
+    // offs[b]: pages needed by the sequences before b
+    uint32_t* offs = (uint32_t*)kv.region;
+    int32_t* fresh = (int32_t*)(offs + kv.slots);
+    uint32_t want = 0;
+    bool full_row = false;
+    for (uint32_t base = 0; base < batch.n; base += kPlanThreads) {
+        const uint32_t b = base + threadIdx.x;
+        uint32_t need = 0, total;
+        if (b < batch.n) {
+            const int slot = batch.slot(b, kv.slots);
+            if (slot >= 0) {
+                const int len = __ldcg(kv.lens + slot), rows = batch.count(b);
+                need = blocks_of(kv, len + rows) - blocks_of(kv, len);
+                full_row |= (uint64_t)max(0, len) + rows > (uint64_t)kv.width << kv.page_shift;
+            }
+        }
+        const uint32_t at = want + block_scan(need, &total);
+        if (b < batch.n && blockIdx.x == 0) offs[b] = at;
+        want += total;
+    }
+    const uint32_t got = take_lowest_free(kv, want, fresh, kv.head->part);
+    if (blockIdx.x == 0 && (full_row || (got < want && threadIdx.x == 0))) atomicOr(&kv.head->status, kKvStatNoPages);
+    cluster_barrier();
+    const uint32_t lane = threadIdx.x & 31u;
+    for (uint32_t b = plan_rank() >> 5; b < batch.n; b += kPlanCtas * kPlanThreads / 32u) {
+        const int slot = batch.slot(b, kv.slots);
+        if (slot < 0) continue;
+        const int len = __ldcg(kv.lens + slot), rows = batch.count(b);
+        const uint32_t from = blocks_of(kv, len), to = blocks_of(kv, len + rows), off = __ldcg(offs + b);
+        for (uint32_t i = from + lane; i < to; i += 32u) {
+            const uint32_t r = off + i - from;
+            kv.table[(uint64_t)slot * kv.width + i] = r < got ? __ldcg(fresh + r) : -1;
+        }
+        __syncwarp();
+        if (lane == 0) kv.lens[slot] = len + rows;
+    }
+}
+
+// ---------------------------------------------------------------------------------- fork
+
+// Rows of the new tables wait in the region ([n][width]) until every src has been read.
+__global__ void __launch_bounds__(kPlanThreads) fork_kernel(Kv kv, const int32_t* src, const int32_t* dst, uint32_t n)
+{
+    int32_t* rows = (int32_t*)kv.region;
+    int32_t* new_len = rows + (uint64_t)kv.slots * kv.width;
+    int32_t* fresh = new_len + kv.slots;
+    int32_t* tail = fresh + kv.slots;         // [n] page that is copied for pair i, -1: none
+    int32_t* pair_from = tail + kv.slots;
+    int32_t* pair_to = pair_from + kv.pages;
+    const uint32_t lane = threadIdx.x & 31u, warps = kPlanCtas * kPlanThreads / 32u;
+    auto live = [&](uint32_t i, int* s, int* d) {
+        *s = __ldg(src + i);
+        *d = __ldg(dst + i);
+        return *s != *d && (uint32_t)*s < kv.slots && (uint32_t)*d < kv.slots;
+    };
+    // the new rows, one more reference for each of their pages (a tail page is held until the copies are planned)
+    for (uint32_t i = plan_rank() >> 5; i < n; i += warps) {
+        int s, d;
+        if (!live(i, &s, &d)) {
+            if (lane == 0) tail[i] = -1;
+            continue;
+        }
+        const int len = max(0, __ldcg(kv.lens + s));
+        const uint32_t whole = min(kv.width, (uint32_t)len >> kv.page_shift), used = blocks_of(kv, len);
+        for (uint32_t e = lane; e < kv.width; e += 32u) {
+            int p = e < used ? __ldcg(kv.table + (uint64_t)s * kv.width + e) : -1;
+            if ((uint32_t)p >= kv.pages) p = -1;
+            if (p >= 0) atomicAdd(kv.refs + p, 1);
+            rows[(uint64_t)i * kv.width + e] = p;
+            if (e == whole && used > whole) tail[i] = p;
+        }
+        if (lane == 0) {
+            if (used <= whole) tail[i] = -1;
+            new_len[i] = len;
+        }
+    }
+    cluster_barrier();
+    // what the targets held is released
+    for (uint32_t i = plan_rank() >> 5; i < n; i += warps) {
+        int s, d;
+        if (!live(i, &s, &d)) continue;
+        const uint32_t used = blocks_of(kv, __ldcg(kv.lens + d));
+        for (uint32_t e = lane; e < used; e += 32u) {
+            const int p = __ldcg(kv.table + (uint64_t)d * kv.width + e);
+            if ((uint32_t)p < kv.pages) atomicSub(kv.refs + p, 1);
+        }
+    }
+    uint32_t want = 0;
+    for (uint32_t base = 0; base < n; base += kPlanThreads) {
+        uint32_t total;
+        const uint32_t i = base + threadIdx.x;
+        block_scan(i < n && __ldcg(tail + i) >= 0, &total);
+        want += total;
+    }
+    cluster_barrier();
+    const uint32_t got = take_lowest_free(kv, want, fresh, kv.head->part);
+    cluster_barrier();
+    // pairs in the order of i; the held tail pages are let go
+    if (blockIdx.x == 0) {
+        uint32_t at0 = 0;
+        for (uint32_t base = 0; base < n; base += kPlanThreads) {
+            const uint32_t i = base + threadIdx.x;
+            const int t = i < n ? __ldcg(tail + i) : -1;
+            uint32_t total;
+            const uint32_t at = at0 + block_scan(t >= 0, &total);
+            if (t >= 0) {
+                const int to = at < got ? __ldcg(fresh + at) : -1;
+                atomicSub(kv.refs + t, 1);
+                if (to >= 0) {
+                    pair_from[at] = t;
+                    pair_to[at] = to;
+                }
+                rows[(uint64_t)i * kv.width + ((uint32_t)__ldcg(new_len + i) >> kv.page_shift)] = to;
+            }
+            at0 += total;
+        }
+        if (threadIdx.x == 0) {
+            kv.head->pairs = got;
+            if (got < want) atomicOr(&kv.head->status, kKvStatNoPages);
+        }
+    }
+    cluster_barrier();
+    for (uint32_t i = plan_rank() >> 5; i < n; i += warps) {
+        int s, d;
+        if (!live(i, &s, &d)) continue;
+        for (uint32_t e = lane; e < kv.width; e += 32u)
+            kv.table[(uint64_t)d * kv.width + e] = __ldcg(rows + (uint64_t)i * kv.width + e);
+        if (lane == 0) kv.lens[d] = __ldcg(new_len + i);
+    }
+}
+
+// ---------------------------------------------------------------------------------- free, trim
+
+// One warp per slot.  trim = false: everything; else the pages whose tokens all lie at or before
+// len - 1 - window and none of which is a sink.
+__global__ void __launch_bounds__(256) release_kernel(Kv kv, const int32_t* slots, uint32_t n, bool trim, uint32_t window,
+                                                      uint32_t sinks)
+{
+    const uint32_t i = (blockIdx.x * 256u + threadIdx.x) >> 5, lane = threadIdx.x & 31u;
+    if (i >= n) return;
+    const int slot = __ldg(slots + i);
+    if ((uint32_t)slot >= kv.slots) return;
+    const int len = kv.lens[slot];
+    __syncwarp();                       // every lane has the length before lane 0 clears it
+    uint32_t from = 0, to = blocks_of(kv, len);
+    if (trim) {
+        const int64_t gone = (int64_t)len - window;         // tokens before this one are outside every later window
+        from = (uint32_t)min((uint64_t)kv.width, ((uint64_t)sinks + kv.page() - 1u) >> kv.page_shift);
+        to = gone > 0 ? min(to, (uint32_t)(gone >> kv.page_shift)) : 0u;
+    }
+    for (uint32_t e = from + lane; e < to; e += 32u) {
+        int32_t* at = kv.table + (uint64_t)slot * kv.width + e;
+        const int p = *at;
+        if ((uint32_t)p < kv.pages) atomicSub(kv.refs + p, 1);
+        *at = -1;
+    }
+    if (!trim && lane == 0) kv.lens[slot] = 0;
+}
+
+// ---------------------------------------------------------------------------------- compact
+
+__global__ void __launch_bounds__(kPlanThreads) compact_kernel(Kv kv)
+{
+    int32_t* from = (int32_t*)kv.region;      // [pages] pages that move, ascending
+    int32_t* to = from + kv.pages;            // [pages] free places that they go to, ascending
+    int32_t* moved = to + kv.pages;           // [pages] new place of a page
+    uint32_t lo, hi, before, live, holes_before, holes, movers_before, movers;
+    segment(kv.pages, &lo, &hi);
+    auto is_live = [&](uint32_t p) { return __ldcg(kv.refs + p) > 0; };
+    const uint32_t mine = count_pages(lo, hi, is_live);
+    uint32_t* part = kv.head->part;
+    if (threadIdx.x == 0) part[blockIdx.x] = mine;
+    cluster_barrier();
+    part_sums(part, &before, &live);
+    const uint32_t low_hi = min(hi, max(lo, live)), high_lo = max(lo, min(hi, live));
+    const uint32_t free_low = (low_hi - lo) - count_pages(lo, low_hi, is_live);
+    const uint32_t live_high = count_pages(high_lo, hi, is_live);
+    if (threadIdx.x == 0) {
+        part[kPlanCtas + blockIdx.x] = free_low;
+        part[2 * kPlanCtas + blockIdx.x] = live_high;
+    }
+    cluster_barrier();
+    part_sums(part + kPlanCtas, &holes_before, &holes);
+    part_sums(part + 2 * kPlanCtas, &movers_before, &movers);
+    rank_pages(lo, low_hi, holes_before, holes, [&](uint32_t p) { return !is_live(p); },
+               [&](uint32_t rank, uint32_t p) { to[rank] = (int32_t)p; });
+    rank_pages(high_lo, hi, movers_before, movers, is_live, [&](uint32_t rank, uint32_t p) { from[rank] = (int32_t)p; });
+    cluster_barrier();
+    for (uint32_t k = plan_rank(); k < movers; k += kPlanCtas * kPlanThreads) {
+        const int f = __ldcg(from + k), t = __ldcg(to + k);
+        kv.refs[t] = __ldcg(kv.refs + f);
+        kv.refs[f] = 0;
+        moved[f] = t;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) kv.head->pairs = movers;
+    cluster_barrier();
+    if (movers == 0) return;
+    const uint32_t lane = threadIdx.x & 31u;
+    for (uint32_t s = plan_rank() >> 5; s < kv.slots; s += kPlanCtas * kPlanThreads / 32u) {
+        const uint32_t used = blocks_of(kv, __ldg(kv.lens + s));
+        for (uint32_t e = lane; e < used; e += 32u) {
+            int32_t* at = kv.table + (uint64_t)s * kv.width + e;
+            const int p = *at;
+            if (p >= (int)live && (uint32_t)p < kv.pages) *at = __ldcg(moved + p);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------- copies
+
+// Sources and targets of one list never overlap (a target was free, a source in use), so the order does not matter.
+// Pieces of 16 KB are dealt out over the grid: 256 threads, four 16-byte loads in flight each.
+constexpr uint32_t kCopyPiece = 16384;
+
+__global__ void __launch_bounds__(256) copy_pages_kernel(Kv kv, const int32_t* from, const int32_t* to)
+{
+    const uint32_t pairs = __ldcg(&kv.head->pairs);
+    const uint32_t page_bytes = (uint32_t)kv.page_bytes(), pieces = (page_bytes + kCopyPiece - 1u) / kCopyPiece;
+    const uint64_t all = (uint64_t)pairs * pieces;
+    for (uint64_t w = blockIdx.x; w < all; w += gridDim.x) {
+        const uint32_t k = (uint32_t)(w / pieces), piece = (uint32_t)(w - (uint64_t)k * pieces);
+        const int f = __ldg(from + k), t = __ldg(to + k);
+        const uint4* a = (const uint4*)(kv.codes + (uint64_t)f * kv.page_bytes() + (uint64_t)piece * kCopyPiece);
+        uint4* b = (uint4*)(kv.codes + (uint64_t)t * kv.page_bytes() + (uint64_t)piece * kCopyPiece);
+        const uint32_t vectors = min(kCopyPiece, page_bytes - piece * kCopyPiece) / 16u;
+        uint4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (threadIdx.x + 256u * j < vectors) v[j] = __ldcs(a + threadIdx.x + 256u * j);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (threadIdx.x + 256u * j < vectors) __stcs(b + threadIdx.x + 256u * j, v[j]);
+        if (piece == 0)
+            for (uint32_t h = threadIdx.x; h < 2u * kv.heads; h += 256u)
+                kv.scales[(uint64_t)t * 2u * kv.heads + h] = kv.scales[(uint64_t)f * 2u * kv.heads + h];
+    }
+}
+
+template <typename... Args>
+cudaError_t launch_plan(void (*kernel)(Args...), cudaStream_t s, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kPlanCtas);
+    cfg.blockDim = dim3(kPlanThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kPlanCtas;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+entro_status launch_copy(const Kv& kv, const int32_t* from, const int32_t* to, uint64_t most_pairs, cudaStream_t s)
+{
+    Workspace* ws;
+    {
+        Guard g;
+        ws = workspace();
+    }
+    if (!ws) return ENTRO_ERR_CUDA;
+    const uint64_t pieces = most_pairs * ((kv.page_bytes() + kCopyPiece - 1) / kCopyPiece);
+    const uint64_t most = (uint64_t)ws->sm_count * 8u;
+    copy_pages_kernel<<<(unsigned)(pieces < most ? pieces : most), 256, 0, s>>>(kv, from, to);
+    count_launch(2);
+    ENTRO_CUDA(cudaGetLastError());
+    return ENTRO_OK;
+}
+
+}  // namespace
+}  // namespace entro
+
+using namespace entro;
+
+extern "C" uint64_t entro_kv_work_bytes(const entro_kv_cache* c)
+{
+    if (!c || !c->pages || !c->kv_heads || !c->slots || !c->table_width) return 0;
+    if (c->pages >= 0x7fffffffu || c->kv_heads > 1024u || c->slots >= 0x01000000u || c->table_width >= 0x01000000u) return 0;
+    if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128) return 0;
+    if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return 0;
+    // the largest user of the region: fork's rows and lists, or compact's three lists, or reserve's
+    const uint64_t slots = c->slots, pages = c->pages;
+    const uint64_t fork = 4ull * (slots * c->table_width + 3 * slots + 2 * pages);
+    const uint64_t compact = 4ull * 3 * pages;
+    const uint64_t reserve = 4ull * (slots + pages);
+    uint64_t most = fork > compact ? fork : compact;
+    if (reserve > most) most = reserve;
+    return kKvWorkRegion + (most + 255) / 256 * 256;
+}
+
+extern "C" entro_status entro_kv_reserve(const entro_kv_cache* cache, const entro_kv_batch* b, void* cuda_stream)
+{
+    Kv kv;
+    KvBatch batch;
+    if (entro_status e = kv_check(cache, &kv)) return e;
+    if (entro_status e = kv_check(cache, b, &batch)) return e;
+    if (batch.n == 0 || batch.rows == 0) return ENTRO_OK;
+    ENTRO_CUDA(launch_plan(reserve_kernel, (cudaStream_t)cuda_stream, kv, batch));
+    count_launch();
+    return ENTRO_OK;
+}
+
+extern "C" entro_status entro_kv_fork(const entro_kv_cache* cache, const int32_t* src, const int32_t* dst, uint32_t n,
+                                      void* cuda_stream)
+{
+    Kv kv;
+    if (entro_status e = kv_check(cache, &kv)) return e;
+    if (n == 0) return ENTRO_OK;
+    if (!src || !dst || !aligned(src, 4) || !aligned(dst, 4) || n > kv.slots) return ENTRO_ERR_INVALID_ARG;
+    ENTRO_CUDA(launch_plan(fork_kernel, (cudaStream_t)cuda_stream, kv, src, dst, n));
+    const int32_t* from = (const int32_t*)kv.region + (uint64_t)kv.slots * kv.width + 3ull * kv.slots;
+    return launch_copy(kv, from, from + kv.pages, n, (cudaStream_t)cuda_stream);
+}
+
+extern "C" entro_status entro_kv_free(const entro_kv_cache* cache, const int32_t* slots, uint32_t n, void* cuda_stream)
+{
+    Kv kv;
+    if (entro_status e = kv_check(cache, &kv)) return e;
+    if (n == 0) return ENTRO_OK;
+    if (!slots || !aligned(slots, 4) || n > kv.slots) return ENTRO_ERR_INVALID_ARG;
+    release_kernel<<<(n + 7u) / 8u, 256, 0, (cudaStream_t)cuda_stream>>>(kv, slots, n, false, 0u, 0u);
+    count_launch();
+    ENTRO_CUDA(cudaGetLastError());
+    return ENTRO_OK;
+}
+
+extern "C" entro_status entro_kv_trim(const entro_kv_cache* cache, const int32_t* slots, uint32_t n, uint32_t window,
+                                      uint32_t sinks, void* cuda_stream)
+{
+    Kv kv;
+    if (entro_status e = kv_check(cache, &kv)) return e;
+    if (n == 0 || window == 0) return ENTRO_OK;
+    if (!slots || !aligned(slots, 4) || n > kv.slots) return ENTRO_ERR_INVALID_ARG;
+    release_kernel<<<(n + 7u) / 8u, 256, 0, (cudaStream_t)cuda_stream>>>(kv, slots, n, true, window, sinks);
+    count_launch();
+    ENTRO_CUDA(cudaGetLastError());
+    return ENTRO_OK;
+}
+
+extern "C" entro_status entro_kv_compact(const entro_kv_cache* cache, void* cuda_stream)
+{
+    Kv kv;
+    if (entro_status e = kv_check(cache, &kv)) return e;
+    ENTRO_CUDA(launch_plan(compact_kernel, (cudaStream_t)cuda_stream, kv));
+    const int32_t* from = (const int32_t*)kv.region;
+    return launch_copy(kv, from, from + kv.pages, kv.pages / 2u + 1u, (cudaStream_t)cuda_stream);
+}
+
+extern "C" entro_status entro_kv_status(const entro_kv_cache* cache, void* cuda_stream)
+{
+    Kv kv;
+    if (entro_status e = kv_check(cache, &kv)) return e;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    uint32_t st = 0;
+    ENTRO_CUDA(cudaStreamSynchronize(s));
+    ENTRO_CUDA(cudaMemcpyAsync(&st, &kv.head->status, sizeof(st), cudaMemcpyDeviceToHost, s));
+    ENTRO_CUDA(cudaMemsetAsync(&kv.head->status, 0, sizeof(st), s));
+    ENTRO_CUDA(cudaStreamSynchronize(s));
+    if (st & kKvStatInternal) return ENTRO_ERR_UNSUPPORTED;
+    if (st & kKvStatNoPages) return ENTRO_ERR_NO_PAGES;
+    return st ? ENTRO_ERR_NONFINITE : ENTRO_OK;
+}

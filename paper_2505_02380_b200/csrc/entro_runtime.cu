@@ -174,6 +174,7 @@ extern "C" const char* entro_status_string(entro_status st)
         case ENTRO_ERR_CUDA: return "a CUDA call failed";
         case ENTRO_ERR_UNSUPPORTED: return "unsupported";
         case ENTRO_ERR_TOO_MANY_TENSORS: return "more tensors than the static scratch holds";
+        case ENTRO_ERR_NO_PAGES: return "the key/value cache has no page left";
     }
     return "unknown status";
 }

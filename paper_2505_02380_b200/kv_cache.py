@@ -1,0 +1,217 @@
+"""Binding of the key/value cache calls (include/entro.h, entro_kv_*): marshalling only.
+
+A token step calls these once per layer, so the argument blocks are packed with one
+struct.pack_into per call into memory that the handle keeps, instead of building ctypes
+structures field by field.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import struct
+from typing import Optional, Tuple
+
+import torch
+
+import paper_2505_02380_b200 as _E
+
+KV_ZERO_POINT = 128
+_TYPES = {torch.float16: 0, torch.bfloat16: 1}
+_CACHE = struct.Struct("=6QQ6I")        # entro_kv_cache
+_BATCH = struct.Struct("=2I2Q")         # entro_kv_batch
+_ROWS = struct.Struct("=2Q4q2i")        # entro_kv_rows
+_QUERY = struct.Struct("=3Q4q4Ifi")     # entro_kv_query
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+class KvCache:
+    """The key/value cache of one layer: the caller's tensors and their argument block.
+
+    codes  uint8   [pages, 2, kv_heads, page_tokens, head_dim]  (keys, values)
+    scales float32 [pages, 2, kv_heads]
+    table  int32   [slots, table_width], -1 for no page;  lens int32 [slots];  refs int32 [pages]
+    work:  uint8 device memory of entro_kv_work_bytes, zero; allocated here unless another cache's
+    (KvCache.work) is given, which is allowed where the two caches' calls do not overlap on the GPU.
+    """
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                 refs: torch.Tensor, work: Optional[torch.Tensor] = None):
+        if codes.dim() != 5 or codes.shape[1] != 2:
+            raise ValueError("codes: [pages, 2, kv_heads, page_tokens, head_dim]")
+        pages, _, heads, page, dim = codes.shape
+        if tuple(scales.shape) != (pages, 2, heads) or table.dim() != 2 or tuple(refs.shape) != (pages,) \
+                or tuple(lens.shape) != (table.shape[0],):
+            raise ValueError("scales, table, lens and refs do not fit codes")
+        self.codes, self.scales, self.table, self.lens, self.refs = codes, scales, table, lens, refs
+        self.pages, self.kv_heads, self.page_tokens, self.head_dim = pages, heads, page, dim
+        self.slots, self.table_width = table.shape
+        self.device = codes.device
+        self._dev = codes.device.index
+        blocks = C.create_string_buffer(256)
+        self._blocks = blocks
+        self._cache = C.addressof(blocks)
+        self._batch, self._args = self._cache + 96, self._cache + 128
+        ptrs = (_E._dev(codes, torch.uint8), _E._dev(scales, torch.float32), _E._dev(table, torch.int32),
+                _E._dev(lens, torch.int32), _E._dev(refs, torch.int32))
+        sizes = (pages, heads, page, dim, self.slots, self.table_width)
+        _CACHE.pack_into(blocks, 0, *ptrs, 0, 0, *sizes)
+        L = _E.lib()
+        need = int(L.entro_kv_work_bytes(self._cache))
+        if need == 0:
+            raise _E.EntroError(_E.ERR_UNSUPPORTED, "KvCache")
+        if work is None:
+            work = torch.zeros(need, dtype=torch.uint8, device=codes.device)
+        self.work = work
+        _CACHE.pack_into(blocks, 0, *ptrs, _E._dev(work, torch.uint8), work.numel(), *sizes)
+        self._attention, self._append, self._read = L.entro_kv_attention, L.entro_kv_append, L.entro_kv_read
+
+    def _set_batch(self, rows: int, slots: Optional[torch.Tensor], row_start: Optional[torch.Tensor]) -> None:
+        if row_start is not None:
+            n = row_start.shape[0] - 1
+            start = row_start.data_ptr()
+            if row_start.dtype != torch.int32 or not row_start.is_cuda or not row_start.is_contiguous():
+                raise ValueError("row_start: contiguous int32 device tensor")
+        else:
+            n, start = rows, 0
+        if slots is not None:
+            if slots.dtype != torch.int32 or not slots.is_cuda or not slots.is_contiguous() or slots.shape[0] != n:
+                raise ValueError("slots: contiguous int32 device tensor, one entry per sequence")
+            _BATCH.pack_into(self._blocks, 96, n, rows, slots.data_ptr(), start)
+        else:
+            _BATCH.pack_into(self._blocks, 96, n, rows, 0, start)
+
+    def _stream(self, stream: Optional[torch.cuda.Stream]) -> int:
+        return stream.cuda_stream if stream is not None else _raw_stream(self._dev)
+
+
+def _check(status: int, what: str) -> None:
+    if status:
+        raise _E.EntroError(status, what)
+
+
+def _rows_of(t: torch.Tensor, heads: int, dim: int, what: str) -> Tuple[int, int, int]:
+    """(rows, row stride, head stride) of a [rows, heads, dim] device tensor whose last dimension is contiguous."""
+    shape, stride = t.shape, t.stride()
+    if not t.is_cuda or len(shape) != 3 or shape[1] != heads or shape[2] != dim or stride[2] != 1:
+        raise ValueError(f"{what}: [rows, {heads}, {dim}] on the device, last dimension contiguous")
+    return shape[0], stride[0], stride[1]
+
+
+def entro_kv_create(pages: int, kv_heads: int, head_dim: int, page_tokens: int, slots: int, max_tokens: int,
+                    device="cuda", work: Optional[torch.Tensor] = None) -> KvCache:
+    """An empty cache: `pages` pages, `slots` sequences of at most max_tokens tokens each."""
+    device = torch.device(device)
+    if device.index is None:
+        device = torch.device(device.type, torch.cuda.current_device())
+    width = max(1, -(-max_tokens // page_tokens))
+    return KvCache(torch.full((pages, 2, kv_heads, page_tokens, head_dim), KV_ZERO_POINT, dtype=torch.uint8, device=device),
+                   torch.zeros(pages, 2, kv_heads, device=device),
+                   torch.full((slots, width), -1, dtype=torch.int32, device=device),
+                   torch.zeros(slots, dtype=torch.int32, device=device),
+                   torch.zeros(pages, dtype=torch.int32, device=device), work)
+
+
+def entro_kv_reserve(kv: KvCache, rows: Optional[int] = None, slots: Optional[torch.Tensor] = None,
+                     row_start: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Grow the sequences by their rows and give them the pages they need.  rows: total number of rows
+    (not needed with row_start, whose last entry it is, or with slots, one row each).  Asynchronous."""
+    if rows is None:
+        # the kernel takes each sequence's rows from row_start; the bound only has to be no smaller
+        rows = 0x7fffffff if row_start is not None else slots.shape[0]
+    kv._set_batch(rows, slots, row_start)
+    _check(_E.lib().entro_kv_reserve(kv._cache, kv._batch, kv._stream(stream)), "entro_kv_reserve")
+
+
+def _pack_rows(kv: KvCache, k: torch.Tensor, v: torch.Tensor) -> int:
+    rows, kr, kh = _rows_of(k, kv.kv_heads, kv.head_dim, "k")
+    rows_v, vr, vh = _rows_of(v, kv.kv_heads, kv.head_dim, "v")
+    if rows != rows_v or k.dtype != v.dtype or k.dtype not in _TYPES:
+        raise ValueError("k and v: the same number of rows, both float16 or both bfloat16")
+    _ROWS.pack_into(kv._blocks, 128, k.data_ptr(), v.data_ptr(), kr, kh, vr, vh, _TYPES[k.dtype], 0)
+    return rows
+
+
+def entro_kv_append(kv: KvCache, k: torch.Tensor, v: torch.Tensor, slots: Optional[torch.Tensor] = None,
+                    row_start: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Quantise the rows k, v [rows, kv_heads, head_dim] (any strides that are multiples of 8) and write them
+    to the sequences' last positions.  row_start int32 [n + 1], or None: one row per sequence.  Asynchronous."""
+    kv._set_batch(_pack_rows(kv, k, v), slots, row_start)
+    _check(kv._append(kv._cache, kv._batch, kv._args, kv._stream(stream)), "entro_kv_append")
+
+
+def entro_kv_read(kv: KvCache, rows: Optional[int] = None, slots: Optional[torch.Tensor] = None,
+                  row_start: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float16,
+                  k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None):
+    """-> (k, v): the last rows of every sequence as the cache holds them.  Asynchronous."""
+    if k is None or v is None:
+        k = torch.empty(rows, kv.kv_heads, kv.head_dim, dtype=dtype, device=kv.device)
+        v = torch.empty_like(k)
+    kv._set_batch(_pack_rows(kv, k, v), slots, row_start)
+    _check(kv._read(kv._cache, kv._batch, kv._args, kv._stream(stream)), "entro_kv_read")
+    return k, v
+
+
+def entro_kv_attention(kv: KvCache, q: torch.Tensor, slots: Optional[torch.Tensor] = None,
+                       row_start: Optional[torch.Tensor] = None, max_rows: int = 0, softmax_scale: float = 0.0,
+                       window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None,
+                       lse: Optional[torch.Tensor] = None, return_lse: bool = False,
+                       stream: Optional[torch.cuda.Stream] = None):
+    """Attention of the rows q [rows, q_heads, head_dim] over the sequences, whose last tokens they are.
+    softmax_scale 0: 1 / sqrt(head_dim).  window 0: none.  max_rows: no sequence brings more rows (0: not known).
+    -> out, or (out, lse) where lse float32 [rows, q_heads] is given or asked for.  Asynchronous."""
+    heads = q.shape[1]
+    rows, qr, qh = _rows_of(q, heads, kv.head_dim, "q")
+    if out is None:
+        out = torch.empty(rows, heads, kv.head_dim, dtype=q.dtype, device=q.device)
+    out_rows, orow, oh = _rows_of(out, heads, kv.head_dim, "out")
+    if lse is None and return_lse:
+        lse = torch.empty(rows, heads, dtype=torch.float32, device=q.device)
+    if out_rows != rows or out.dtype != q.dtype or q.dtype not in _TYPES:
+        raise ValueError("q and out: the same shape, both float16 or both bfloat16")
+    lse_at = 0
+    if lse is not None:
+        if lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.shape != (rows, heads):
+            raise ValueError("lse: contiguous float32 [rows, q_heads] on the device")
+        lse_at = lse.data_ptr()
+    kv._set_batch(rows, slots, row_start)
+    _QUERY.pack_into(kv._blocks, 128, q.data_ptr(), out.data_ptr(), lse_at, qr, qh, orow, oh, heads, max_rows, window,
+                     sinks, softmax_scale, _TYPES[q.dtype])
+    _check(kv._attention(kv._cache, kv._batch, kv._args, kv._stream(stream)), "entro_kv_attention")
+    return out if lse is None else (out, lse)
+
+
+def _slot_list(t: torch.Tensor) -> Tuple[int, int]:
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or t.dim() != 1:
+        raise ValueError("slots: contiguous int32 device tensor")
+    return t.data_ptr(), t.shape[0]
+
+
+def entro_kv_fork(kv: KvCache, src: torch.Tensor, dst: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Slot dst[i] becomes a copy of slot src[i]: full pages are shared, the last one is copied.  Asynchronous."""
+    (s, n), (d, m) = _slot_list(src), _slot_list(dst)
+    if n != m:
+        raise ValueError("src and dst: the same length")
+    _check(_E.lib().entro_kv_fork(kv._cache, s, d, n, kv._stream(stream)), "entro_kv_fork")
+
+
+def entro_kv_free(kv: KvCache, slots: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Release the slots' pages; their lengths become 0.  Asynchronous."""
+    p, n = _slot_list(slots)
+    _check(_E.lib().entro_kv_free(kv._cache, p, n, kv._stream(stream)), "entro_kv_free")
+
+
+def entro_kv_trim(kv: KvCache, slots: torch.Tensor, window: int, sinks: int = 0,
+                  stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Release the pages that no row from the last position on sees with this window and these sinks.  Asynchronous."""
+    p, n = _slot_list(slots)
+    _check(_E.lib().entro_kv_trim(kv._cache, p, n, window, sinks, kv._stream(stream)), "entro_kv_trim")
+
+
+def entro_kv_compact(kv: KvCache, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Move the live pages to the front of the pool.  Asynchronous."""
+    _check(_E.lib().entro_kv_compact(kv._cache, kv._stream(stream)), "entro_kv_compact")
+
+
+def entro_kv_status(kv: KvCache, stream: Optional[torch.cuda.Stream] = None) -> int:
+    """Synchronises; OK, ERR_NO_PAGES or ERR_NONFINITE since the last call."""
+    return int(_E.lib().entro_kv_status(kv._cache, kv._stream(stream)))

@@ -3,6 +3,7 @@ and its host-only entry points agree with the oracle.  No kernel runs here."""
 import ctypes as C
 import os
 import re
+import struct
 
 import numpy as np
 import pytest
@@ -128,3 +129,64 @@ def test_argument_errors_are_found_before_any_launch():
     assert L.entro_decode_dequant(16, 100, 16, 16, 4096, C.byref(bad), 1.0, 0, 32, None) == E.ERR_INVALID_ARG
     assert L.entro_decode_dequant_batched(None, 3, None) == E.ERR_INVALID_ARG
     assert L.entro_decode_dequant_batched(None, 0, None) == E.OK
+
+
+def _kv_cache(**changes):
+    """An entro_kv_cache block with made-up addresses (no call that passes its checks is made with it)."""
+    f = dict(codes=4096, scales=4096, table=4096, lens=4096, refs=4096, work=4096, work_bytes=1 << 30, pages=100, heads=8, page=16,
+             dim=64, slots=10, width=20)
+    f.update(changes)
+    buf = C.create_string_buffer(128)
+    struct.pack_into("=7Q6I", buf, 0, *f.values())
+    return buf
+
+
+def test_kv_cache_refusals_before_any_launch():
+    L = E.lib()
+    batch = struct.pack("=2I2Q", 2, 2, 4096, 0)
+    rows = struct.pack("=2Q4q2i", 4096, 4096, 512, 64, 512, 64, 0, 0)
+    query = struct.pack("=3Q4q4Ifi", 4096, 4096, 0, 512, 64, 512, 64, 8, 0, 0, 0, 0.0, 0)
+
+    def calls(cache, batch=batch, rows=rows, query=query):
+        return [L.entro_kv_reserve(cache, batch, None), L.entro_kv_append(cache, batch, rows, None),
+                L.entro_kv_read(cache, batch, rows, None), L.entro_kv_attention(cache, batch, query, None)]
+
+    for change in (dict(codes=0), dict(codes=4100), dict(scales=0), dict(scales=4098), dict(table=0), dict(lens=0), dict(refs=0),
+                   dict(work=0), dict(work=4104), dict(pages=0), dict(heads=0), dict(slots=0), dict(width=0), dict(pages=1 << 31)):
+        cache = _kv_cache(**change)
+        assert set(calls(cache)) == {E.ERR_INVALID_ARG}, change
+        assert L.entro_kv_free(cache, 4096, 1, None) == E.ERR_INVALID_ARG
+        assert L.entro_kv_fork(cache, 4096, 4096, 1, None) == E.ERR_INVALID_ARG
+        assert L.entro_kv_trim(cache, 4096, 1, 8, 0, None) == E.ERR_INVALID_ARG
+        assert L.entro_kv_compact(cache, None) == E.ERR_INVALID_ARG
+    for change in (dict(page=17), dict(page=256), dict(page=8), dict(dim=80), dict(dim=256), dict(dim=32)):
+        assert set(calls(_kv_cache(**change))) == {E.ERR_UNSUPPORTED}, change
+        assert L.entro_kv_work_bytes(_kv_cache(**change)) == 0
+    assert set(calls(_kv_cache(work_bytes=4096))) == {E.ERR_BUFFER_TOO_SMALL}
+    assert set(calls(None)) == {E.ERR_INVALID_ARG} and L.entro_kv_work_bytes(None) == 0
+    good = _kv_cache()
+    # more sequences than slots, rows that do not fit one row each, unaligned lists
+    for b in (struct.pack("=2I2Q", 11, 11, 4096, 0), struct.pack("=2I2Q", 2, 3, 4096, 0), struct.pack("=2I2Q", 2, 2, 4097, 0),
+              struct.pack("=2I2Q", 2, 9, 4096, 4098), struct.pack("=2I2Q", 2, 1 << 31, 4096, 4096)):
+        assert set(calls(good, batch=b)) == {E.ERR_INVALID_ARG}
+    assert set(calls(good, batch=None)) == {E.ERR_INVALID_ARG}
+    for r in ((0, 4096, 512, 64, 512, 64, 0, 0), (4096, 0, 512, 64, 512, 64, 0, 0), (4104, 4096, 512, 64, 512, 64, 0, 0),
+              (4096, 4096, 513, 64, 512, 64, 0, 0), (4096, 4096, 512, 64, 512, 65, 0, 0), (4096, 4096, 512, 64, 512, 64, 2, 0),
+              (4096, 4096, 512, 64, 512, 64, 0, 1)):
+        r = struct.pack("=2Q4q2i", *r)
+        assert L.entro_kv_append(good, batch, r, None) == L.entro_kv_read(good, batch, r, None) == E.ERR_INVALID_ARG
+    for q in ((0, 4096, 0, 512, 64, 512, 64, 8, 0, 0, 0, 0.0, 0), (4096, 0, 0, 512, 64, 512, 64, 8, 0, 0, 0, 0.0, 0),
+              (4096, 4096, 2, 512, 64, 512, 64, 8, 0, 0, 0, 0.0, 0), (4096, 4096, 0, 512, 63, 512, 64, 8, 0, 0, 0, 0.0, 0),
+              (4096, 4096, 0, 512, 64, 511, 64, 8, 0, 0, 0, 0.0, 0), (4096, 4096, 0, 512, 64, 512, 64, 0, 0, 0, 0, 0.0, 0),
+              (4096, 4096, 0, 512, 64, 512, 64, 12, 0, 0, 0, 0.0, 0), (4096, 4096, 0, 512, 64, 512, 64, 8, 0, 0, 0, -1.0, 0),
+              (4096, 4096, 0, 512, 64, 512, 64, 8, 0, 0, 0, float("nan"), 0),
+              (4096, 4096, 0, 512, 64, 512, 64, 8, 0, 0, 0, float("inf"), 0), (4096, 4096, 0, 512, 64, 512, 64, 8, 0, 0, 0, 0.0, 2)):
+        assert L.entro_kv_attention(good, batch, struct.pack("=3Q4q4Ifi", *q), None) == E.ERR_INVALID_ARG, q
+    assert L.entro_kv_fork(good, None, 4096, 1, None) == L.entro_kv_fork(good, 4096, 4096, 11, None) == E.ERR_INVALID_ARG
+    assert L.entro_kv_free(good, None, 1, None) == L.entro_kv_free(good, 4098, 1, None) == E.ERR_INVALID_ARG
+    assert L.entro_kv_trim(good, 4096, 11, 8, 0, None) == E.ERR_INVALID_ARG
+    # nothing to do is not an error
+    nothing = struct.pack("=2I2Q", 0, 0, 0, 0)
+    assert set(calls(good, batch=nothing)) == {E.OK}
+    assert L.entro_kv_free(good, None, 0, None) == L.entro_kv_fork(good, None, None, 0, None) == E.OK
+    assert "page" in E.status_string(E.ERR_NO_PAGES)
