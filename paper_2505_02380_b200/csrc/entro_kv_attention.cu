@@ -1,17 +1,10 @@
 // Attention over the paged 8-bit key/value cache.
-#include "entro_kv_common.cuh"
+#include "entro_kv_attention.cuh"
+
+#include "entro_kv_tokens.cuh"
 
 namespace entro {
 namespace {
-
-struct Query {
-    const unsigned char* q;
-    unsigned char* out;
-    float* lse;
-    int64_t q_row, q_head, out_row, out_head;    // strides in bytes
-    uint32_t heads, group, window, sinks;
-    float scale;
-};
 
 // One warp per row and query head, token after token: a lane holds dim / 32 of the values.
 template <typename T, int kDim>
@@ -64,15 +57,33 @@ __global__ void __launch_bounds__(128) attention_simple_kernel(Kv kv, KvBatch ba
 }
 
 template <typename T>
-void launch_simple(const Kv& kv, const KvBatch& batch, const Query& q, cudaStream_t s)
+entro_status launch_attention(const Kv& kv, const KvBatch& batch, const Query& q, uint32_t max_rows, cudaStream_t s)
 {
-    const dim3 grid(batch.rows, (q.heads + 3u) / 4u);
-    if (kv.dim == 64)
-        attention_simple_kernel<T, 64><<<grid, 128, 0, s>>>(kv, batch, q);
-    else if (kv.dim == 96)
-        attention_simple_kernel<T, 96><<<grid, 128, 0, s>>>(kv, batch, q);
-    else
-        attention_simple_kernel<T, 128><<<grid, 128, 0, s>>>(kv, batch, q);
+    Workspace* ws;
+    {
+        Guard g;
+        ws = workspace();
+    }
+    if (!ws) return ENTRO_ERR_CUDA;
+    const uint64_t rows = (uint64_t)(batch.row_start ? (max_rows ? max_rows : batch.rows) : 1u) * q.group;
+    if (rows <= kTokenRows) {
+        float* partials = (float*)kv.region;
+        cudaError_t e = kv.dim == 64   ? launch_tokens<T, 64>(kv, batch, q, (uint32_t)rows, (uint32_t)ws->sm_count, partials, s)
+                        : kv.dim == 96 ? launch_tokens<T, 96>(kv, batch, q, (uint32_t)rows, (uint32_t)ws->sm_count, partials, s)
+                                       : launch_tokens<T, 128>(kv, batch, q, (uint32_t)rows, (uint32_t)ws->sm_count, partials, s);
+        ENTRO_CUDA(e);
+    } else {
+        const dim3 grid(batch.rows, (q.heads + 3u) / 4u);
+        if (kv.dim == 64)
+            attention_simple_kernel<T, 64><<<grid, 128, 0, s>>>(kv, batch, q);
+        else if (kv.dim == 96)
+            attention_simple_kernel<T, 96><<<grid, 128, 0, s>>>(kv, batch, q);
+        else
+            attention_simple_kernel<T, 128><<<grid, 128, 0, s>>>(kv, batch, q);
+        ENTRO_CUDA(cudaGetLastError());
+    }
+    count_launch();
+    return ENTRO_OK;
 }
 
 }  // namespace
@@ -108,11 +119,6 @@ extern "C" entro_status entro_kv_attention(const entro_kv_cache* cache, const en
     q.window = a->window;
     q.sinks = a->sinks;
     q.scale = a->softmax_scale > 0.f ? a->softmax_scale : 1.f / sqrtf((float)kv.dim);
-    if (a->type == ENTRO_FLOAT16)
-        launch_simple<__half>(kv, batch, q, (cudaStream_t)cuda_stream);
-    else
-        launch_simple<__nv_bfloat16>(kv, batch, q, (cudaStream_t)cuda_stream);
-    count_launch();
-    ENTRO_CUDA(cudaGetLastError());
-    return ENTRO_OK;
+    return a->type == ENTRO_FLOAT16 ? launch_attention<__half>(kv, batch, q, a->max_rows, (cudaStream_t)cuda_stream)
+                                    : launch_attention<__nv_bfloat16>(kv, batch, q, a->max_rows, (cudaStream_t)cuda_stream);
 }

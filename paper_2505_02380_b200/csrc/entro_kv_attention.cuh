@@ -1,0 +1,123 @@
+// What the attention kernels on the paged 8-bit cache share: the query side of a call, how the work
+// of a ragged batch is cut into equal shares, and how partial results of a split unit are joined.
+//
+// Mathematics.  With codes k', v' (value = scale * code, code = byte - 128), key scale a_b and value
+// scale c_b of the page b a token lies in, everything in units of log2:
+//   t_j = (q . k'_j) * a_b * softmax_scale * log2(e)
+//   u_j = t_j + log2(c_b),   M = running max of u_j,   P_j = 2^(u_j - M)  in [0, 1]
+//   out = sum_j P_j v'_j / L,   L = sum_j P_j / c_b,   lse = ln 2 * (M + log2 L).
+// The value scale rides in the exponent, so the second product works on the bare codes (exact in
+// fp16) and costs no multiplication per element, and P_j is rounded to fp16 relative to the largest
+// term of the sum it enters.  So that u_j is no larger than t_j (its rounding would show in lse),
+// c_b is taken relative to a power of two near the value scale of the first page that the unit sees;
+// out gets that power back.  No scale is 0 (the smallest is 2^-60), so the division is safe; a page
+// whose values are 2^100 times smaller than another's would lose its weight in L.
+#pragma once
+
+#include "entro_kv_common.cuh"
+
+namespace entro {
+
+struct Query {
+    const unsigned char* q;
+    unsigned char* out;
+    float* lse;
+    int64_t q_row, q_head, out_row, out_head;    // strides in bytes
+    uint32_t heads, group, window, sinks;
+    float scale;
+};
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr uint32_t kCodeToHalf = 0x64646464u;    // fp16 0x64uu = 1024 + u: a byte becomes a number by placing it
+constexpr uint32_t kHalfBias = 0x64806480u;      // 1024 + 128
+
+__device__ __forceinline__ uint32_t sub_half2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// bytes 0, 1 (low) or 2, 3 (high) of a word of codes as two fp16 numbers, exactly
+__device__ __forceinline__ uint32_t codes_low(uint32_t w) { return sub_half2(__byte_perm(w, kCodeToHalf, 0x4140), kHalfBias); }
+__device__ __forceinline__ uint32_t codes_high(uint32_t w) { return sub_half2(__byte_perm(w, kCodeToHalf, 0x4342), kHalfBias); }
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float lg2(float x)
+{
+    float r;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float rcp(float x)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Power of two that brings a bf16 query row with largest magnitude `top` into fp16's range, exactly:
+// the largest value to about 2^14; eight significant bits stay whole down to 2^-30 of it.
+__device__ __forceinline__ int row_exponent(float top)
+{
+    if (!(top > 0.f) || top > 3.4e38f) return 0;
+    const int e = (int)(__float_as_uint(top) >> 23) - 127;
+    return min(126, 14 - e);
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// The power of two near the value scale of block `block` of a sequence (1 where there is none).
+__device__ __forceinline__ float value_reference(const Kv& kv, int slot, uint32_t block, uint32_t head)
+{
+    const int page = slot >= 0 ? kv_page(kv, slot, block) : -1;
+    if (page < 0) return 1.f;
+    const float c = __ldg(kv.scales + ((uint64_t)(uint32_t)page * 2u + 1u) * kv.heads + head);
+    return c >= 1e-30f && c <= 1e37f ? __uint_as_float(__float_as_uint(c) & 0x7f800000u) : 1.f;
+}
+// A value scale relative to it (by_ref = 1 / reference).  A page that nothing was written to has scale 0.
+__device__ __forceinline__ float relative_scale(float c, float by_ref) { return fminf(fmaxf(c * by_ref, 1e-35f), 1e35f); }
+
+// The part of a sequence that its rows see, in pieces of 2^shift tokens: pieces 0 .. sinks - 1, then low, low + 1, ...
+struct Span {
+    uint32_t sinks, low, count;      // count = all pieces
+    __device__ __forceinline__ uint32_t piece(uint32_t i) const { return i < sinks ? i : low + (i - sinks); }
+};
+
+// Rows at positions first .. last (last >= 0).
+__device__ __forceinline__ Span span_of(int first, int last, uint32_t window, uint32_t sinks, uint32_t shift)
+{
+    const uint32_t end = ((uint32_t)last >> shift) + 1u;
+    uint32_t low = 0;
+    if (window) {
+        const int64_t near = (int64_t)first - (int64_t)window + 1;
+        if (near > 0) low = (uint32_t)(near >> shift);
+    }
+    const uint32_t kept = (uint32_t)min((uint64_t)low, ((uint64_t)sinks + (1u << shift) - 1u) >> shift);
+    return Span{kept, low, kept + end - low};
+}
+
+__device__ __forceinline__ bool sees(int position, int j, uint32_t window, uint32_t sinks)
+{
+    return j <= position && (window == 0u || (int64_t)j > (int64_t)position - (int64_t)window || (uint32_t)j < sinks);
+}
+
+// x pieces of work in equal shares for `parts` blocks: the first `more` get one more.
+struct Shares {
+    uint32_t each, more;
+    __device__ __forceinline__ Shares(uint32_t all, uint32_t parts) : each(all / parts), more(all % parts) {}
+    __device__ __forceinline__ uint32_t start(uint32_t c) const { return c * each + min(c, more); }
+    __device__ __forceinline__ uint32_t owner(uint32_t x) const
+    {
+        const uint32_t big = more * (each + 1u);
+        return x < big ? x / (each + 1u) : more + (x - big) / each;
+    }
+};
+
+}  // namespace
+}  // namespace entro

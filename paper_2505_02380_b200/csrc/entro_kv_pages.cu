@@ -398,13 +398,14 @@ extern "C" uint64_t entro_kv_work_bytes(const entro_kv_cache* c)
     if (c->pages >= 0x7fffffffu || c->kv_heads > 1024u || c->slots >= 0x01000000u || c->table_width >= 0x01000000u) return 0;
     if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128) return 0;
     if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return 0;
-    // the largest user of the region: fork's rows and lists, or compact's three lists, or reserve's
+    // the largest user of the region: fork's rows and lists, compact's three lists, reserve's, or attention's partial results
     const uint64_t slots = c->slots, pages = c->pages;
     const uint64_t fork = 4ull * (slots * c->table_width + 3 * slots + 2 * pages);
     const uint64_t compact = 4ull * 3 * pages;
     const uint64_t reserve = 4ull * (slots + pages);
     uint64_t most = fork > compact ? fork : compact;
     if (reserve > most) most = reserve;
+    if (kKvPartialBytes > most) most = kKvPartialBytes;
     return kKvWorkRegion + (most + 255) / 256 * 256;
 }
 
