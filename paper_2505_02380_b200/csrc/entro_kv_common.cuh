@@ -21,8 +21,9 @@ struct KvWorkHeader {
 };
 constexpr uint64_t kKvWorkRegion = (sizeof(KvWorkHeader) + 255) / 256 * 256;
 
-// Room for attention's partial results: 512 blocks, two each, 16 rows of at most 128 + 2 floats.
-constexpr uint64_t kKvPartialBytes = 512ull * 2 * 16 * 130 * 4;
+// Room for attention's partial results.  Single tokens: 512 blocks, two each, 16 rows of at most 128 + 2 floats;
+// prompts: 160 blocks, two each, 256 rows.
+constexpr uint64_t kKvPartialBytes = 160ull * 2 * 256 * 130 * 4;
 
 struct Kv {
     uint8_t* codes;
