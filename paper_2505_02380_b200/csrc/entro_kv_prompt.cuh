@@ -6,14 +6,20 @@
 // units form one line that is cut into equal shares, one per SM, and units that are cut are joined by
 // whoever arrives last.
 //
-// One block per SM, warp-specialised around mbarriers:
+// One block of 512 threads per SM, warp-specialised around mbarriers; the launch's registers are shared
+// out again by role:
 //   warps 0 - 3, 4 - 7   softmax of rows 0 - 127 and 128 - 255, one thread per row: reads S from tensor
-//                        memory, writes P over it as fp16, rescales the output sum when its row's
-//                        maximum has grown by more than 2^8, writes results
-//   warps 8 - 11         bytes of the cache to fp16 in shared memory (keys and values, two pieces each)
-//   warp 12, one thread  issues tcgen05.mma:  S = Q K'^T (both in shared memory) and O += P V' (P in
-//                        tensor memory); order QK0(j), PV1(j-1), QK1(j), PV0(j), so that one half's
-//                        products run under the other half's softmax
+//                        memory (twice, for the maximum and for the exponentials: a read costs about 200
+//                        cycles, holding 128 columns would cost the registers of the other roles), writes P
+//                        over it as fp16, rescales the output sum when its row's maximum has grown by more
+//                        than 2^8, writes results
+//   warps 8 - 11         bytes of the cache to fp16 in shared memory (keys and values, two pieces each);
+//                        a piece's bytes are requested while the piece before it is stored
+//   warp 12              issues tcgen05.mma:  S = Q K'^T (both in shared memory) and O += P V' (P in tensor
+//                        memory); order QK0(j), PV1(j-1), QK1(j), PV0(j) without regard to where units end,
+//                        so that one half's products run under the other half's softmax
+//   warps 13 - 15        walk along the share, publish each unit to the others, and bring its rows to shared
+//                        memory as fp16 (three tiles of 128 rows in turn, so one unit ahead)
 // Keys lie [token][dim] and are a K-major operand; values lie [token][dim] too, which is an MN-major
 // operand, so both are stored alike: 128-byte rows of 64 dims, 16-byte units XORed with the row (the
 // 128-byte swizzle of the matrix descriptors).
@@ -25,12 +31,16 @@
 namespace entro {
 namespace {
 
-constexpr uint32_t kPromptThreads = 416;
+constexpr uint32_t kPromptThreads = 512;
 constexpr uint32_t kPromptRows = 256;            // rows of a unit
 constexpr uint32_t kPromptBlocks = 160;          // most blocks of a launch
 constexpr uint32_t kPromptMinPieces = 2;         // a share is not made smaller than this
 constexpr uint32_t kPromptUnitCost = 2;          // starting and ending a unit, in pieces
 constexpr uint32_t kSlabBytes = 128 * 128;       // 128 rows of 64 fp16 numbers
+// Registers a thread of each role (the launch's 512 x 128 are shared out again).  None may spill: with the tiles
+// taking 227 KB little is left of the L1 cache, and a spilled register comes back from L2.
+constexpr int kSoftmaxRegisters = 144, kConvertRegisters = 128, kProductRegisters = 96;
+static_assert(256 * kSoftmaxRegisters + 128 * kConvertRegisters + 128 * kProductRegisters <= 512 * 128, "no more than the launch has");
 constexpr uint32_t kWaitLimit = 1u << 20;        // tries of a barrier wait (each may suspend) before the kernel gives up
 constexpr float kGrowth = 8.f;                   // P stays below 2^8: the output sum is rescaled when the maximum grows by more
 constexpr uint32_t kPromptArrived = 512;         // first counter of KvWorkHeader::arrived that is this kernel's
@@ -38,17 +48,13 @@ constexpr uint32_t kPromptArrived = 512;         // first counter of KvWorkHeade
 template <int kDim>
 constexpr uint32_t kPromptSlabs = kDim == 64 ? 1 : 2;
 template <int kDim>
-constexpr uint32_t kPromptSmem = 1024 + 6 * kPromptSlabs<kDim> * kSlabBytes + 1024;
+constexpr uint32_t kPromptSmem = 7 * kPromptSlabs<kDim> * kSlabBytes + 3072;
+// Dynamic shared memory starts here in the shared window when there is no static part (the first KiB is the driver's);
+// the kernel checks it.  Tile addresses are then constants, and on a 1024-byte boundary as the swizzle wants them.
+constexpr uint32_t kWindow = 1024;
 
 static_assert(kKvPartialBytes >= 4ull * kPromptBlocks * 2 * kPromptRows * 130, "a block leaves at most two partial results");
 
-struct PromptShared {
-    uint64_t q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], scale_full[4];
-    uint64_t joint[2], drained;                  // the warps of a half meet; products of a run that was given up
-    float4 scales[4][8];                         // ring of pieces: per 16 tokens key factor, log2 of the value scale, its inverse
-    uint32_t tmem, dead, last[2];
-};
-static_assert(sizeof(PromptShared) <= 1024, "fits behind the tiles");
 
 // ---------------------------------------------------------------------------------- barriers, tensor memory
 
@@ -62,7 +68,7 @@ __device__ __forceinline__ void bar_arrive(uint64_t* b)
     asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(shared_address(b)) : "memory");
 }
 // One thread's wait; false when it ran out of tries here or in another warp: the caller leaves its loop.
-__device__ __forceinline__ bool bar_wait_one(uint64_t* b, uint32_t parity, PromptShared& sh)
+__device__ __forceinline__ bool bar_wait_one(uint64_t* b, uint32_t parity, uint32_t& dead)
 {
     const uint32_t a = shared_address(b);
     for (uint32_t i = 0; i < kWaitLimit; ++i) {
@@ -73,15 +79,15 @@ __device__ __forceinline__ bool bar_wait_one(uint64_t* b, uint32_t parity, Promp
             : "r"(a), "r"(parity)
             : "memory");
         if (done) return true;
-        if ((i & 63u) == 63u && *(volatile uint32_t*)&sh.dead) return false;
+        if ((i & 63u) == 63u && *(volatile uint32_t*)&dead) return false;
     }
-    *(volatile uint32_t*)&sh.dead = 1u;
+    *(volatile uint32_t*)&dead = 1u;
     return false;
 }
 // A whole warp's wait, the same answer for all lanes.
-__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, PromptShared& sh)
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, uint32_t& dead)
 {
-    return __all_sync(0xffffffffu, bar_wait_one(b, parity, sh));
+    return __all_sync(0xffffffffu, bar_wait_one(b, parity, dead));
 }
 __device__ __forceinline__ void tc_commit(uint64_t* b)
 {
@@ -114,6 +120,13 @@ __device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t (&r)[32])
         "r"(r[31])
         : "memory");
 }
+__device__ __forceinline__ void tm_load16(uint32_t at, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(at));
+}
 __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&r)[16])
 {
     asm volatile(
@@ -122,33 +135,91 @@ __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&r)[16])
         "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+template <int kCount>
+__device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCount)); }
+template <int kCount>
+__device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCount)); }
+// one lane of the warp
+__device__ __forceinline__ bool elected()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0u;
+}
+
+// two float32 operations in one instruction
+__device__ __forceinline__ uint64_t pair(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 __device__ __forceinline__ void tm_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Matrix descriptor of a tile stored as 128-byte rows with the 128-byte swizzle: address, leading offset, 1024 bytes
-// from one group of eight rows to the next (all in 16-byte units), version 1, swizzle mode 2.
-__device__ __forceinline__ uint64_t tile_descriptor(uint32_t address, uint32_t leading_bytes)
+// Bits c of a group of 32 columns with c <= upto and (c > after or c < kept), the group's first column being c0.
+__device__ __forceinline__ uint32_t bits_upto(int c) { return c < 0 ? 0u : c > 30 ? 0xffffffffu : (2u << c) - 1u; }
+__device__ __forceinline__ uint32_t seen_bits(int upto, int after, int kept, int c0)
 {
-    return (uint64_t)((address >> 4) & 0x3fffu) | (uint64_t)((leading_bytes >> 4) & 0x3fffu) << 16 | (uint64_t)(1024u >> 4) << 32 |
-           (uint64_t)1u << 46 | (uint64_t)2u << 61;
+    return bits_upto(upto - c0) & (~bits_upto(after - c0) | bits_upto(kept - 1 - c0));
 }
+__device__ __forceinline__ void hide_unseen(uint32_t (&s)[32], uint32_t seen)
+{
+#pragma unroll
+    for (int e = 0; e < 32; ++e) s[e] = seen & (1u << e) ? s[e] : 0xff800000u;
+}
+
+// Matrix descriptor of a tile stored as 128-byte rows with the 128-byte swizzle.  High word, the same for all tiles
+// here: 1024 bytes from one group of eight rows to the next (in 16-byte units), version 1, swizzle mode 2.  Low word:
+// address and leading offset, in 16-byte units.  Kept apart, so that the one thread that issues products works on
+// 32-bit numbers and stays within its few registers.
+constexpr uint32_t kTileHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
 // Instruction descriptor: fp16 operands, fp32 sums, 128 rows, `n` columns, second operand K-major or MN-major.
 __device__ __forceinline__ constexpr uint32_t product_descriptor(uint32_t n, bool mn_major)
 {
     return 1u << 4 | (mn_major ? 1u << 16 : 0u) | (n >> 3) << 17 | (128u >> 4) << 24;
 }
-__device__ __forceinline__ void tc_product_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t what, uint32_t add)
+// D += A B with both operands in shared memory (`add` false: D = A B)
+__device__ __forceinline__ void tc_product_shared(uint32_t d, uint32_t a, uint32_t b, uint32_t what, uint32_t add)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
-        "l"(b), "r"(what), "r"(add)
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(kTileHigh), "r"(what), "r"(add)
         : "memory");
 }
-__device__ __forceinline__ void tc_product_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t what, uint32_t add)
+// the same with A in tensor memory
+__device__ __forceinline__ void tc_product_tensor(uint32_t d, uint32_t a, uint32_t b, uint32_t what, uint32_t add)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a),
-        "l"(b), "r"(what), "r"(add)
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(kTileHigh), "r"(what), "r"(add)
         : "memory");
 }
 
@@ -190,42 +261,49 @@ __device__ __forceinline__ uint32_t prompt_weight(const PromptSeq& s, const Quer
     return w;
 }
 
-// A block's way along its share; every warp keeps one of its own and they all take the same steps.
+// A unit as its block sees it.
+struct alignas(16) PromptUnit {
+    int slot, len, rows, row0;
+    uint32_t head, tile, from, to;                       // from .. to: the pieces that are this block's
+    Span span;
+    float ref;                                           // value_reference of the unit
+    uint32_t first, end;                                 // line places of the unit's first piece and of its end
+    uint32_t two, there;                                 // more than 128 rows; 0: the share is done
+};
+
+// A block's way along its share of the line.
 struct PromptWalk {
     uint32_t x, end;                 // what is left of the share
     uint32_t b, head, tile, begin;   // the current unit and where it begins on the line
     PromptSeq seq;
-    // of the unit that next() returned
-    Span span;
-    uint32_t from, to;               // pieces of this block
-    uint32_t unit_first, unit_end;   // line places of the unit's first piece and of its end
-    uint32_t unit_head, unit_tile;
-    PromptSeq unit_seq;
-    bool two;                        // more than 128 rows
 
-    __device__ __forceinline__ bool next(const Kv& kv, const KvBatch& batch, const Query& q, uint32_t few_rows)
+    __device__ __forceinline__ void next(const Kv& kv, const KvBatch& batch, const Query& q, uint32_t few_rows, PromptUnit& u)
     {
+        u.there = 0;
         while (x < end) {
             if (seq.tiles == 0) {
                 seq = prompt_seq(kv, batch, q, ++b, few_rows);
                 continue;
             }
-            span = prompt_span(seq, q, tile);
-            unit_first = begin + kPromptUnitCost;
-            unit_end = unit_first + span.count;
-            const uint32_t a = max(x, unit_first), e = min(end, unit_end);
-            const bool some = a < e;
-            unit_head = head;
-            unit_tile = tile;
-            unit_seq = seq;
-            if (some) {
-                from = a - unit_first;
-                to = e - unit_first;
-                two = (uint32_t)seq.rows * q.group - tile * kPromptRows > 128u;
+            u.span = prompt_span(seq, q, tile);
+            u.first = begin + kPromptUnitCost;
+            u.end = u.first + u.span.count;
+            const uint32_t a = max(x, u.first), e = min(end, u.end);
+            if (a < e) {
+                u.there = 1;
+                u.slot = seq.slot;
+                u.len = seq.len;
+                u.rows = seq.rows;
+                u.row0 = seq.row0;
+                u.head = head;
+                u.tile = tile;
+                u.from = a - u.first;
+                u.to = e - u.first;
+                u.two = (uint32_t)seq.rows * q.group - tile * kPromptRows > 128u;
             }
             x = max(x, e);
-            if (x >= unit_end) {
-                begin = unit_end;
+            if (x >= u.end) {
+                begin = u.end;
                 if (++tile == seq.tiles) {
                     tile = 0;
                     if (++head == kv.heads) {
@@ -234,27 +312,39 @@ struct PromptWalk {
                     }
                 }
             }
-            if (some) return true;
+            if (u.there) return;
         }
-        return false;
     }
 };
+
+struct PromptShared {
+    uint64_t q_full[3], q_empty[3], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], scale_full[4];
+    uint64_t unit_full[4], unit_free[4];
+    uint64_t joint[2], drained;                  // the warps of a half meet; products of a run that was given up
+    PromptUnit unit[4];                          // ring of units
+    float4 scales[4][8];                         // ring of pieces: per 16 tokens key factor, log2 of the value scale, its inverse
+    float factor[3][128];                        // per row of the Q tiles: the power of two taken out of it
+    uint32_t seq_weight[64];
+    uint32_t tmem, dead, last[2];
+};
+static_assert(sizeof(PromptShared) <= 3072, "fits behind the tiles");
 
 template <typename T, int kDim>
 __global__ void __launch_bounds__(kPromptThreads, 1)
     prompt_attention_kernel(Kv kv, KvBatch batch, Query q, float* partials, uint32_t few_rows)
 {
-    constexpr uint32_t kSlabs = kPromptSlabs<kDim>, kTile = kSlabs * kSlabBytes;
-    constexpr int kUnits = kDim / 8;             // 16-byte units of a row
-    extern __shared__ unsigned char raw_shared[];
-    unsigned char* tiles = raw_shared + ((1024u - (shared_address(raw_shared) & 1023u)) & 1023u);
-    unsigned char* const q_tile = tiles;                     // [2] tiles
-    unsigned char* const k_tile = tiles + 2 * kTile;         // [2] stages
-    unsigned char* const v_tile = tiles + 4 * kTile;         // [2] stages
-    PromptShared& sh = *(PromptShared*)(tiles + 6 * kTile);
-    __shared__ uint32_t seq_weight[64];
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    constexpr uint32_t kTile = kPromptSlabs<kDim> * kSlabBytes;
+    extern __shared__ __align__(1024) unsigned char tiles[];
+    unsigned char* const k_tile = tiles + 3 * kTile;         // [2] stages; the three Q tiles come first
+    unsigned char* const v_tile = tiles + 5 * kTile;         // [2] stages
+    PromptShared& sh = *(PromptShared*)(tiles + 7 * kTile);
+    uint32_t* const seq_weight = sh.seq_weight;
+    const uint32_t lane = threadIdx.x & 31u, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     constexpr uint32_t kWarps = kPromptThreads / 32u;
+    if (shared_address(tiles) != kWindow) {
+        if (threadIdx.x == 0) atomicOr(&kv.head->status, kKvStatInternal);
+        return;
+    }
 
     // ---- this block's share of the line
     uint32_t all = 0;
@@ -325,8 +415,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
 
     // ---- barriers and tensor memory
     if (threadIdx.x == 0) {
+        for (int i = 0; i < 3; ++i) {
+            bar_init(&sh.q_full[i], 3);          // the loading warps
+            bar_init(&sh.q_empty[i], 5);         // the last product that reads the tile, and the four softmax warps of its rows
+        }
         for (int i = 0; i < 2; ++i) {
-            bar_init(&sh.q_full[i], 4);
             bar_init(&sh.k_full[i], 4);
             bar_init(&sh.k_empty[i], 1);
             bar_init(&sh.v_full[i], 4);
@@ -336,7 +429,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             bar_init(&sh.o_full[i], 1);
             bar_init(&sh.joint[i], 4);
         }
-        for (int i = 0; i < 4; ++i) bar_init(&sh.scale_full[i], 4);
+        for (int i = 0; i < 4; ++i) {
+            bar_init(&sh.scale_full[i], 4);
+            bar_init(&sh.unit_full[i], 1);
+            bar_init(&sh.unit_free[i], 13);      // softmax, converting and product warps
+        }
         bar_init(&sh.drained, 1);
         sh.dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -348,164 +445,141 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
     }
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = sh.tmem;
+    // all 512 columns are this block's, so they start at 0: addresses in tensor memory are constants as well
 
     if (warp < 8u) {
         // =============================================================== softmax, one thread per row
+        registers_up<kSoftmaxRegisters>();
         const uint32_t half = warp >> 2, row = threadIdx.x & 127u;
         const uint32_t lanes = (warp & 3u) << 21;            // lane field of a tensor memory address
-        const uint32_t s_at = tmem + lanes + half * 128u, o_at = tmem + lanes + 256u + half * 128u;
-        unsigned char* my_q = q_tile + half * kTile + row * 128u;
-        uint32_t piece_count = 0, s_count = 0, unit_count = 0;   // pieces of the walk, of this half, units of this half
+        const uint32_t s_at = lanes + half * 128u, o_at = lanes + 256u + half * 128u;
+        uint32_t piece_count = 0, s_count = 0, unit_count = 0;   // pieces of the block, of this half, units of this half
+        uint32_t q_use = 0;                                      // Q tiles used before the unit
         uint32_t joints = 0;                                     // times this half's warps have met
-        bool ok = true;
         auto meet = [&]() {
             __syncwarp();
             if (lane == 0) bar_arrive(&sh.joint[half]);
-            return bar_wait(&sh.joint[half], joints++ & 1u, sh);
+            return bar_wait(&sh.joint[half], joints++ & 1u, sh.dead);
         };
-        while (ok && walk.next(kv, batch, q, few_rows)) {
-            const uint32_t pieces = walk.to - walk.from;
-            if (half && !walk.two) {
+        bool ok = true;
+        for (uint32_t un = 0; ok; ++un) {
+            ok = bar_wait(&sh.unit_full[un & 3u], un >> 2 & 1u, sh.dead);
+            if (!ok) break;
+            const PromptUnit& unit = sh.unit[un & 3u];
+            if (!unit.there) break;
+            const uint32_t pieces = unit.to - unit.from;
+            const uint32_t my_q = q_use + half;
+            q_use += unit.two ? 2u : 1u;
+            if (half && !unit.two) {
                 piece_count += pieces;
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.unit_free[un & 3u]);
                 continue;
             }
-            const PromptSeq& seq = walk.unit_seq;
-            const uint32_t r = walk.unit_tile * kPromptRows + half * 128u + row, rows = (uint32_t)seq.rows * q.group;
+            const uint32_t r0 = unit.tile * kPromptRows + half * 128u, r = r0 + row, rows = (uint32_t)unit.rows * q.group;
             const bool real = r < rows;
-            const int first = seq.len - seq.rows;
+            const int first = unit.len - unit.rows;
             const int position = real ? first + (int)(r / q.group) : -1;
-            const int64_t out_row = seq.row0 + (int)(r / q.group);
-            const uint32_t query_head = walk.unit_head * q.group + r % q.group;
             // positions of the first and last row of this half
-            const uint32_t r0 = walk.unit_tile * kPromptRows + half * 128u;
             const int low_position = first + (int)(r0 / q.group), high_position = first + (int)(min(rows - 1u, r0 + 127u) / q.group);
 
-            // the row into shared memory, as fp16
             float row_factor = q.scale * kLog2e;
-            {
-                const uint4* from = (const uint4*)(q.q + out_row * q.q_row + (int64_t)query_head * q.q_head);
-                float up = 1.f;
-                if constexpr (!__is_same(T, __half)) {
-                    float top = 0.f;
-                    if (real) {
-#pragma unroll
-                        for (int u = 0; u < kUnits; ++u) {
-                            const uint4 v = __ldg(from + u);
-                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float2 f = to_float2<T>(w[e]);
-                                top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
-                            }
-                        }
-                    }
-                    const int e = row_exponent(top);
-                    up = power_of_two(e);
-                    row_factor *= power_of_two(-e);
-                }
-#pragma unroll
-                for (int u = 0; u < kUnits; ++u) {
-                    uint4 v = real ? __ldg(from + u) : make_uint4(0u, 0u, 0u, 0u);
-                    if constexpr (!__is_same(T, __half)) {
-                        uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float2 f = to_float2<T>(w[e]);
-                            w[e] = from_float2<__half>(f.x * up, f.y * up);
-                        }
-                        v = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                    *(uint4*)(my_q + (u >> 3) * kSlabBytes + (((uint32_t)u & 7u) ^ (row & 7u)) * 16u) = v;
-                }
-                proxy_fence();
-                __syncwarp();
-                if (lane == 0) bar_arrive(&sh.q_full[half]);
-            }
+            ok = bar_wait(&sh.q_full[my_q % 3u], my_q / 3u & 1u, sh.dead);
+            if (!ok) break;
+            if constexpr (!__is_same(T, __half)) row_factor *= sh.factor[my_q % 3u][row];
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sh.q_empty[my_q % 3u]);
 
             float m = -INFINITY, l = 0.f;
             for (uint32_t j = 0; j < pieces; ++j, ++piece_count, ++s_count) {
                 __syncwarp();
                 const uint32_t ring = piece_count & 3u;
-                const int t0 = (int)(walk.span.piece(walk.from + j) * 128u);
+                const int t0 = (int)(unit.span.piece(unit.from + j) * 128u);
                 const bool whole = t0 + 127 <= low_position &&
                                    (q.window == 0u || (int64_t)t0 > (int64_t)high_position - (int64_t)q.window || (uint32_t)t0 + 127u < q.sinks);
-                // columns that this row sees: up to `upto`, and behind `after` or before `sinks`
-                const int upto = max(-1, min(127, position - t0));
-                const int after = q.window ? (int)max((int64_t)-1, min((int64_t)127, (int64_t)position - (int64_t)q.window - t0)) : -1;
-                const int kept = (int)max((int64_t)0, min((int64_t)128, (int64_t)q.sinks - t0));
-                ok = bar_wait(&sh.scale_full[ring], (piece_count >> 2) & 1u, sh) && bar_wait(&sh.s_full[half], s_count & 1u, sh);
+                ok = bar_wait(&sh.scale_full[ring], (piece_count >> 2) & 1u, sh.dead) && bar_wait(&sh.s_full[half], s_count & 1u, sh.dead);
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t s[32];
+                // columns that this row sees: up to `upto`, and behind `after` or before `kept`
+                int upto = 127, after = -1, kept = 0;
+                if (!whole) {
+                    upto = max(-1, min(127, position - t0));
+                    if (q.window) after = (int)max((int64_t)-1, min((int64_t)127, (int64_t)position - (int64_t)q.window - t0));
+                    kept = (int)max((int64_t)0, min((int64_t)128, (int64_t)q.sinks - t0));
+                }
                 float top = -INFINITY;
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    tm_load32(s_at + 32u * c, s);
+                for (int c = 0; c < 4; c += 2) {
+                    uint32_t s[2][32];
+                    tm_load32(s_at + 32u * c, s[0]);
+                    tm_load32(s_at + 32u * c + 32u, s[1]);
                     tm_wait_load();
                     if (!whole) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const int col = 32 * c + e;
-                            if (!(col <= upto && (col > after || col < kept))) s[e] = 0xff800000u;
-                        }
+                        hide_unseen(s[0], seen_bits(upto, after, kept, 32 * c));
+                        hide_unseen(s[1], seen_bits(upto, after, kept, 32 * c + 32));
                     }
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float4 sc = sh.scales[ring][2 * c + h];
-                        float best = __uint_as_float(s[16 * h]);
+                    for (int h = 0; h < 4; ++h) {
+                        const float2 sc = *(const float2*)&sh.scales[ring][2 * c + h];
+                        float best = __uint_as_float(s[h >> 1][16 * (h & 1)]);
 #pragma unroll
-                        for (int e = 1; e < 16; ++e) best = fmaxf(best, __uint_as_float(s[16 * h + e]));
+                        for (int e = 1; e < 16; ++e) best = fmaxf(best, __uint_as_float(s[h >> 1][16 * (h & 1) + e]));
                         // a factor of 0 times minus infinity would be NaN
                         top = fmaxf(top, best == -INFINITY ? -INFINITY : fmaf(best, sc.x * row_factor, sc.y));
                     }
                 }
-                if (top > m + kGrowth || (m == -INFINITY && top > -INFINITY)) {
-                    // handled below: the maximum moves
-                } else {
-                    top = m;
-                }
-                const float shrink = top == m ? 1.f : ex2(m - top);
-                if (__any_sync(0xffffffffu, top != m) && j > 0) {
+                // the maximum moves when it has grown by more than kGrowth, or from nothing
+                if (!(top > m + kGrowth || (m == -INFINITY && top > -INFINITY))) top = m;
+                if (__any_sync(0xffffffffu, top != m)) {
+                    const float shrink = top == m ? 1.f : ex2(m - top);
+                    l *= shrink;
+                    m = top;
+                    if (j > 0) {
+                        const uint64_t by = pair(shrink, shrink);
 #pragma unroll 1
-                    for (int c = 0; c < kDim / 32; ++c) {
-                        tm_load32(o_at + 32u * c, s);
-                        tm_wait_load();
+                        for (int c = 0; c < kDim / 16; ++c) {
+                            uint32_t o[16];
+                            tm_load16(o_at + 16u * c, o);
+                            tm_wait_load();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * shrink);
-                        tm_store32(o_at + 32u * c, s);
+                            for (int e = 0; e < 16; e += 2) {
+                                const float2 v = unpair(mul2(pair(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), by));
+                                o[e] = __float_as_uint(v.x);
+                                o[e + 1] = __float_as_uint(v.y);
+                            }
+                            tm_store16(o_at + 16u * c, o);
+                        }
                     }
                 }
-                l *= shrink;
-                m = top;
                 const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    tm_load32(s_at + 32u * c, s);
+                for (int c = 0; c < 4; c += 2) {
+                    uint32_t s[2][32], p[32];
+                    tm_load32(s_at + 32u * c, s[0]);
+                    tm_load32(s_at + 32u * c + 32u, s[1]);
                     tm_wait_load();
                     if (!whole) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const int col = 32 * c + e;
-                            if (!(col <= upto && (col > after || col < kept))) s[e] = 0xff800000u;
-                        }
+                        hide_unseen(s[0], seen_bits(upto, after, kept, 32 * c));
+                        hide_unseen(s[1], seen_bits(upto, after, kept, 32 * c + 32));
                     }
-                    uint32_t p[16];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                    for (int h = 0; h < 4; ++h) {
                         const float4 sc = sh.scales[ring][2 * c + h];
                         const float f = fmaxf(sc.x * row_factor, 1e-37f), add = sc.y - base;   // not 0, for the masked ones' sake
-                        float sum = 0.f;
+                        const uint64_t ff = pair(f, f), aa = pair(add, add);
+                        uint64_t sum = 0ull;
 #pragma unroll
                         for (int e = 0; e < 16; e += 2) {
-                            const float a = ex2(fmaf(__uint_as_float(s[16 * h + e]), f, add));
-                            const float b = ex2(fmaf(__uint_as_float(s[16 * h + e + 1]), f, add));
-                            sum += a + b;
+                            const int at = 16 * (h & 1) + e;
+                            const float2 t = unpair(fma2(pair(__uint_as_float(s[h >> 1][at]), __uint_as_float(s[h >> 1][at + 1])), ff, aa));
+                            const float a = ex2(t.x), b = ex2(t.y);
+                            sum = add2(sum, pair(a, b));
                             p[8 * h + e / 2] = from_float2<__half>(a, b);
                         }
-                        l = fmaf(sum, sc.z, l);
+                        const float2 both = unpair(sum);
+                        l = fmaf(both.x + both.y, sc.z, l);
                     }
-                    tm_store16(s_at + 16u * c, p);
+                    tm_store32(s_at + 16u * c, p);      // over columns that have been read
                 }
                 tm_wait_store();
                 tc_fence_before();
@@ -513,23 +587,25 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 if (lane == 0) bar_arrive(&sh.p_full[half]);
             }
             if (!ok) break;
-            ok = bar_wait(&sh.o_full[half], unit_count & 1u, sh);
+            ok = bar_wait(&sh.o_full[half], unit_count & 1u, sh.dead);
             if (!ok) break;
             tc_fence_after();
             ++unit_count;
 
             // ---- results
-            const bool complete = pieces == walk.span.count;
-            const float ref = value_reference(kv, seq.slot, walk.span.piece(0) << (7u - kv.page_shift), walk.unit_head);
+            const bool complete = pieces == unit.span.count;
+            const float ref = unit.ref;
+            const int64_t out_row = unit.row0 + (int)(r / q.group);
+            const uint32_t query_head = unit.head * q.group + r % q.group;
             constexpr uint32_t kPartial = kPromptRows * (kDim + 2u);
-            float* mine = partials + (uint64_t)(blockIdx.x * 2u + (walk.from == 0u ? 1u : 0u)) * kPartial + (half * 128u + row) * kDim;
+            float* mine = partials + (uint64_t)(blockIdx.x * 2u + (unit.from == 0u ? 1u : 0u)) * kPartial + (half * 128u + row) * kDim;
             float* mine_stat = mine - (half * 128u + row) * kDim + kPromptRows * kDim + (half * 128u + row) * 2u;
             unsigned char* out = q.out + out_row * q.out_row + (int64_t)query_head * q.out_head;
             float* lse = q.lse && real ? q.lse + (uint64_t)out_row * q.heads + query_head : nullptr;
             const float by = l == 0.f ? 0.f : ref * __frcp_rn(l);
-            uint32_t o[32];
 #pragma unroll 1
             for (int c = 0; c < kDim / 32; ++c) {
+                uint32_t o[32];
                 __syncwarp();
                 tm_load32(o_at + 32u * c, o);
                 tm_wait_load();
@@ -554,10 +630,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             tc_fence_before();
             if (complete) {
                 if (lse) *lse = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.unit_free[un & 3u]);
                 continue;
             }
             if (real) __stcg((float2*)mine_stat, make_float2(m, l));
-            const uint32_t c0 = shares.owner(walk.unit_first), c1 = shares.owner(walk.unit_end - 1u);
+            const uint32_t c0 = shares.owner(unit.first), c1 = shares.owner(unit.end - 1u);
             __threadfence();
             ok = meet();
             if (!ok) break;
@@ -583,30 +661,38 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 }
                 const float f = sum == 0.f ? 0.f : ref * __frcp_rn(sum);
 #pragma unroll 1
-                for (int d = 0; d < kDim; d += 8) {
-                    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                for (int d = 0; d < kDim; d += 32) {
+                    float v[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = 0.f;
                     for (uint32_t c = c0; c <= c1; ++c) {
                         const float* p = place(c);
+                        float4 a[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) a[e] = __ldcg((const float4*)(p + at * kDim + d) + e);
                         const float w = ex2(__ldcg(p + kPromptRows * kDim + at * 2u) - base);
-                        const float4 a = __ldcg((const float4*)(p + at * kDim + d)), b = __ldcg((const float4*)(p + at * kDim + d + 4));
-                        v[0] = fmaf(a.x, w, v[0]);
-                        v[1] = fmaf(a.y, w, v[1]);
-                        v[2] = fmaf(a.z, w, v[2]);
-                        v[3] = fmaf(a.w, w, v[3]);
-                        v[4] = fmaf(b.x, w, v[4]);
-                        v[5] = fmaf(b.y, w, v[5]);
-                        v[6] = fmaf(b.z, w, v[6]);
-                        v[7] = fmaf(b.w, w, v[7]);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            v[4 * e] = fmaf(a[e].x, w, v[4 * e]);
+                            v[4 * e + 1] = fmaf(a[e].y, w, v[4 * e + 1]);
+                            v[4 * e + 2] = fmaf(a[e].z, w, v[4 * e + 2]);
+                            v[4 * e + 3] = fmaf(a[e].w, w, v[4 * e + 3]);
+                        }
                     }
-                    *(uint4*)(out + 2u * d) = make_uint4(from_float2<T>(v[0] * f, v[1] * f), from_float2<T>(v[2] * f, v[3] * f),
-                                                         from_float2<T>(v[4] * f, v[5] * f), from_float2<T>(v[6] * f, v[7] * f));
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8)
+                        *(uint4*)(out + 2u * (d + e)) =
+                            make_uint4(from_float2<T>(v[e] * f, v[e + 1] * f), from_float2<T>(v[e + 2] * f, v[e + 3] * f),
+                                       from_float2<T>(v[e + 4] * f, v[e + 5] * f), from_float2<T>(v[e + 6] * f, v[e + 7] * f));
                 }
                 if (lse) *lse = sum == 0.f ? -INFINITY : kLn2 * (top + log2f(sum));
             }
             ok = meet();             // last[] has been read
+            if (lane == 0) bar_arrive(&sh.unit_free[un & 3u]);
         }
     } else if (warp < 12u) {
         // =============================================================== cache bytes to fp16 tiles
+        registers_down<kConvertRegisters>();
         const uint32_t w = warp - 8u;
         // eight lanes of a quarter warp write rows {0, 1, 4, 5} or {2, 3, 6, 7} of two neighbouring chunks: under the
         // swizzle that is eight different 16-byte bank groups
@@ -614,32 +700,69 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         const uint32_t chunk = (lane & 1u) | (lane >> 4) << 1;
         constexpr int kHalves = kDim == 64 ? 1 : 2;                              // 64-byte parts of a cache row
         const bool in_second = kDim != 96 || chunk < 2u;
-        uint32_t count = 0;                                                      // pieces of the walk
-        bool ok = true;
-        uint4 kb[4][kHalves], vb[4][kHalves];
-        float key_scale = 0.f, value_scale = 0.f;
-        int page[2] = {-1, -1};
-        uint32_t inside[2] = {0u, 0u};
-        auto find = [&](uint32_t piece) {
-            const PromptSeq& seq = walk.unit_seq;
+        // a piece whose pages have been looked up: two ahead of the piece that is stored, one ahead of its loads
+        struct Place {
+            int page[2];             // of the warp's two groups of 16 tokens
+            uint32_t inside, head;   // first token's place in its page (the second's is 16 further, in the same or the next page)
+            float by_ref;
+            bool there;
+        };
+        uint32_t un = 0, ahead = 0, ahead_end = 0;
+        bool done = false;
+        auto look_up = [&]() {
+            Place p;
+            p.there = false;
+            p.page[0] = p.page[1] = -1;
+            p.inside = p.head = 0u;
+            p.by_ref = 1.f;
+            if (done) return p;
+            const PromptUnit& unit = sh.unit[un & 3u];
+            if (ahead == ahead_end) {
+                if (!bar_wait(&sh.unit_full[un & 3u], un >> 2 & 1u, sh.dead) || !unit.there) {
+                    done = true;
+                    return p;
+                }
+                ahead = unit.from;
+                ahead_end = unit.to;
+            }
+            const uint32_t token = unit.span.piece(ahead++) * 128u + w * 32u;
+            p.there = true;
+            p.head = unit.head;
+            p.by_ref = __frcp_rn(unit.ref);
+            p.inside = token & (kv.page() - 1u);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t token = piece * 128u + w * 32u + h * 16u;
-                page[h] = seq.slot >= 0 && token < (uint32_t)seq.len ? kv_page(kv, seq.slot, token >> kv.page_shift) : -1;
-                inside[h] = token & (kv.page() - 1u);
+                const uint32_t t = token + h * 16u;
+                p.page[h] = unit.slot >= 0 && t < (uint32_t)unit.len ? kv_page(kv, unit.slot, t >> kv.page_shift) : -1;
             }
+            if (ahead == ahead_end) {
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.unit_free[un & 3u]);
+                ++un;
+            }
+            return p;
         };
-        auto load = [&](uint4(&to)[4][kHalves], uint32_t which) {
+        auto load = [&](uint4(&to)[4][kHalves], const Place& p, uint32_t which) {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int p = page[g >> 1];
-                const uint8_t* at = kv.codes + (uint64_t)(uint32_t)max(p, 0) * kv.page_bytes() +
-                                    (uint64_t)(which * kv.heads + walk.unit_head) * kv.head_bytes() +
-                                    (inside[g >> 1] + 8u * (g & 1) + sub_row) * kDim + chunk * 16u;
+                const int page = p.page[g >> 1];
+                const uint32_t inside = (p.inside + 16u * (g >> 1)) & (kv.page() - 1u);
+                const uint8_t* at = kv.codes + (uint64_t)(uint32_t)max(page, 0) * kv.page_bytes() +
+                                    (uint64_t)(which * kv.heads + p.head) * kv.head_bytes() +
+                                    (inside + 8u * (g & 1) + sub_row) * kDim + chunk * 16u;
 #pragma unroll
                 for (int h = 0; h < kHalves; ++h)
-                    to[g][h] = p >= 0 && (h == 0 || in_second) ? __ldg((const uint4*)(at + 64u * h))
-                                                               : make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
+                    to[g][h] = page >= 0 && (h == 0 || in_second) ? __ldg((const uint4*)(at + 64u * h))
+                                                                  : make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
+            }
+        };
+        float key_scale = 0.f, value_scale = 0.f;      // lanes 0, 1: of the warp's groups of 16 tokens
+        auto load_scales = [&](const Place& p) {
+            const int page = lane ? p.page[1] : p.page[0];
+            if (lane < 2u && page >= 0) {
+                const float* at = kv.scales + (uint64_t)(uint32_t)page * 2u * kv.heads + p.head;
+                key_scale = __ldg(at);
+                value_scale = __ldg(at + kv.heads);
             }
         };
         auto store = [&](const uint4(&from)[4][kHalves], unsigned char* tile) {
@@ -658,116 +781,202 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             proxy_fence();
             __syncwarp();
         };
-        while (ok && walk.next(kv, batch, q, few_rows)) {
-            const float by_ref =
-                __frcp_rn(value_reference(kv, walk.unit_seq.slot, walk.span.piece(0) << (7u - kv.page_shift), walk.unit_head));
-            for (uint32_t j = walk.from; j < walk.to; ++j, ++count) {
-                find(walk.span.piece(j));
-                load(kb, 0u);
-                load(vb, 1u);
-                if (lane < 2u) {
-                    const int p = lane ? page[1] : page[0];
-                    if (p >= 0) {
-                        const float* at = kv.scales + (uint64_t)(uint32_t)p * 2u * kv.heads + walk.unit_head;
-                        key_scale = __ldg(at);
-                        value_scale = __ldg(at + kv.heads);
-                    }
-                }
-                const uint32_t stage = count & 1u, parity = (count >> 1 & 1u) ^ 1u;
-                ok = bar_wait(&sh.k_empty[stage], parity, sh);
-                if (!ok) break;
+        uint4 kb[4][kHalves], vb[4][kHalves];
+        Place now, next = look_up();
+        now.there = false;           // the first turn only requests
+        for (uint32_t count = 0; next.there || now.there;) {
+            const uint32_t stage = count & 1u, parity = (count >> 1 & 1u) ^ 1u;
+            if (now.there) {
+                if (!bar_wait(&sh.k_empty[stage], parity, sh.dead)) break;
                 if (lane < 2u) {
                     // the scales of a piece four places back are no longer read: its S tiles have been followed by newer ones
-                    const int p = lane ? page[1] : page[0];
-                    const float rel = relative_scale(value_scale, by_ref);
-                    sh.scales[count & 3u][2u * w + lane] =
-                        p >= 0 ? make_float4(key_scale, lg2(rel), rcp(rel), 0.f) : make_float4(0.f, -INFINITY, 0.f, 0.f);
+                    const float rel = relative_scale(value_scale, now.by_ref);
+                    sh.scales[count & 3u][2u * w + lane] = (lane ? now.page[1] : now.page[0]) >= 0
+                                                               ? make_float4(key_scale, lg2(rel), rcp(rel), 0.f)
+                                                               : make_float4(0.f, -INFINITY, 0.f, 0.f);
                 }
                 store(kb, k_tile + stage * kTile);
                 if (lane == 0) {
                     bar_arrive(&sh.scale_full[count & 3u]);
                     bar_arrive(&sh.k_full[stage]);
                 }
-                ok = bar_wait(&sh.v_empty[stage], parity, sh);
-                if (!ok) break;
+            }
+            load(kb, next, 0u);
+            load_scales(next);
+            if (now.there) {
+                if (!bar_wait(&sh.v_empty[stage], parity, sh.dead)) break;
                 store(vb, v_tile + stage * kTile);
                 if (lane == 0) bar_arrive(&sh.v_full[stage]);
+                ++count;
             }
+            load(vb, next, 1u);
+            now = next;
+            next = look_up();
+        }
+    } else if (warp == 12u) {
+        // =============================================================== products
+        registers_down<kProductRegisters>();
+        constexpr uint32_t kQ = kWindow, kK = kWindow + 3u * kTile, kV = kWindow + 5u * kTile;
+        const bool leader = elected();
+        auto scores = [&](uint32_t half, uint32_t q_buffer, uint32_t stage) {
+            const uint32_t a = (kQ >> 4 | 1u << 16) + q_buffer * (kTile >> 4), b = (kK >> 4 | 1u << 16) + stage * (kTile >> 4);
+            if (leader) {
+#pragma unroll
+                for (uint32_t k = 0; k < kDim / 16; ++k) {
+                    const uint32_t off = ((k >> 2) * kSlabBytes + (k & 3u) * 32u) >> 4;
+                    tc_product_shared(half * 128u, a + off, b + off, product_descriptor(128u, false), k > 0u);
+                }
+                tc_commit(&sh.s_full[half]);
+            }
+            __syncwarp();
+        };
+        auto outputs = [&](uint32_t half, uint32_t stage, bool add) {
+            const uint32_t b = (kV >> 4 | (kSlabBytes >> 4) << 16) + stage * (kTile >> 4);
+            if (leader) {
+#pragma unroll
+                for (uint32_t k = 0; k < 8u; ++k)
+                    tc_product_tensor(256u + half * 128u, half * 128u + 8u * k, b + (2048u >> 4) * k, product_descriptor(kDim, true),
+                                      k > 0u || add);
+            }
+            __syncwarp();
+        };
+        auto commit = [&](uint64_t* b) {
+            if (leader) tc_commit(b);
+            __syncwarp();
+        };
+        uint32_t count = 0, p_use[2] = {0u, 0u}, q_use = 0;
+        bool pending = false, pending_add = false, pending_last = false;     // half 1's second product of the piece before
+        bool ok = true;
+        for (uint32_t un = 0; ok; ++un) {
+            ok = bar_wait(&sh.unit_full[un & 3u], un >> 2 & 1u, sh.dead);
+            if (!ok) break;
+            const PromptUnit& unit = sh.unit[un & 3u];
+            const uint32_t there = __shfl_sync(0xffffffffu, unit.there, 0), two = __shfl_sync(0xffffffffu, unit.two, 0);
+            // after the last unit one more turn issues what is pending
+            const uint32_t pieces = there ? __shfl_sync(0xffffffffu, unit.to - unit.from, 0) : pending ? 1u : 0u;
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sh.unit_free[un & 3u]);
+            const uint32_t use = q_use;
+            q_use += two ? 2u : 1u;
+            for (uint32_t j = 0; ok && j < pieces; ++j) {
+                const uint32_t stage = count & 1u, parity = count >> 1 & 1u;
+                const bool last = j + 1u == pieces;
+                if (there) ok = bar_wait(&sh.k_full[stage], parity, sh.dead);
+                // QK0, PV1 of the piece before, QK1, PV0
+#pragma unroll 1
+                for (uint32_t half = 0; ok && half < 2u; ++half) {
+                    if (there && (half == 0u || two)) {
+                        const uint32_t q_now = use + half;
+                        if (j == 0u) {
+                            ok = bar_wait(&sh.q_full[q_now % 3u], q_now / 3u & 1u, sh.dead);
+                            if (!ok) break;
+                        }
+                        tc_fence_after();
+                        scores(half, q_now % 3u, stage);
+                        if (last) commit(&sh.q_empty[q_now % 3u]);
+                    }
+                    if (half == 1u && there) commit(&sh.k_empty[stage]);
+                    if (half ? there != 0u : pending) {
+                        const uint32_t of = half ^ 1u, v_stage = half ? stage : stage ^ 1u;
+                        const bool ends = half ? last : pending_last;
+                        ok = (!half || bar_wait(&sh.v_full[stage], parity, sh.dead)) && bar_wait(&sh.p_full[of], p_use[of]++ & 1u, sh.dead);
+                        if (!ok) break;
+                        tc_fence_after();
+                        outputs(of, v_stage, half ? j > 0u : pending_add);
+                        if (of == 1u || !two) commit(&sh.v_empty[v_stage]);
+                        if (ends) commit(&sh.o_full[of]);
+                    }
+                    if (half == 0u) pending = false;
+                }
+                if (there && two) {
+                    pending = true;
+                    pending_add = j > 0u;
+                    pending_last = last;
+                }
+                if (there) ++count;
+            }
+            if (!there) break;
+        }
+        if (!ok) {               // given up: say so, and let the products that were issued end
+            if (lane == 0) atomicOr(&kv.head->status, kKvStatInternal);
+            commit(&sh.drained);
+            sh.dead = 0;
+            bar_wait(&sh.drained, 0u, sh.dead);
         }
     } else {
-        // =============================================================== products, one thread
-        if (lane == 0) {
-            const uint32_t q_at = shared_address(q_tile), k_at = shared_address(k_tile), v_at = shared_address(v_tile);
-            auto scores = [&](uint32_t half, uint32_t stage) {
-#pragma unroll
-                for (int k = 0; k < kDim / 16; ++k) {
-                    const uint32_t off = (uint32_t)(k >> 2) * kSlabBytes + (uint32_t)(k & 3) * 32u;
-                    tc_product_shared(tmem + half * 128u, tile_descriptor(q_at + half * kTile + off, 16u),
-                                      tile_descriptor(k_at + stage * kTile + off, 16u), product_descriptor(128u, false), k > 0);
-                }
-            };
-            auto outputs = [&](uint32_t half, uint32_t stage, bool add) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    tc_product_tensor(tmem + 256u + half * 128u, tmem + half * 128u + 8u * k,
-                                      tile_descriptor(v_at + stage * kTile + 2048u * k, kSlabBytes), product_descriptor(kDim, true),
-                                      k > 0 || add);
-            };
-            uint32_t count = 0, s_count[2] = {0u, 0u}, units[2] = {0u, 0u};
-            bool ok = true;
-            while (ok && walk.next(kv, batch, q, few_rows)) {
-                const uint32_t pieces = walk.to - walk.from;
-                const bool two = walk.two;
-                ok = bar_wait_one(&sh.q_full[0], units[0]++ & 1u, sh) && (!two || bar_wait_one(&sh.q_full[1], units[1]++ & 1u, sh));
-                for (uint32_t j = 0; ok && j < pieces; ++j, ++count) {
-                    const uint32_t stage = count & 1u, parity = count >> 1 & 1u;
-                    ok = bar_wait_one(&sh.k_full[stage], parity, sh);
-                    if (!ok) break;
-                    tc_fence_after();
-                    scores(0u, stage);
-                    tc_commit(&sh.s_full[0]);
-                    if (two) {
-                        if (j > 0) {
-                            ok = bar_wait_one(&sh.p_full[1], s_count[1]++ & 1u, sh);
-                            if (!ok) break;
-                            tc_fence_after();
-                            outputs(1u, stage ^ 1u, j > 1);
-                            tc_commit(&sh.v_empty[stage ^ 1u]);
-                        }
-                        scores(1u, stage);
-                        tc_commit(&sh.s_full[1]);
-                    }
-                    tc_commit(&sh.k_empty[stage]);
-                    ok = bar_wait_one(&sh.v_full[stage], parity, sh) && bar_wait_one(&sh.p_full[0], s_count[0]++ & 1u, sh);
-                    if (!ok) break;
-                    tc_fence_after();
-                    outputs(0u, stage, j > 0);
-                    if (!two) tc_commit(&sh.v_empty[stage]);
-                    if (j + 1u == pieces) tc_commit(&sh.o_full[0]);
-                }
-                if (ok && two) {
-                    ok = bar_wait_one(&sh.p_full[1], s_count[1]++ & 1u, sh);
-                    if (!ok) break;
-                    tc_fence_after();
-                    outputs(1u, (count - 1u) & 1u, pieces > 1u);
-                    tc_commit(&sh.v_empty[(count - 1u) & 1u]);
-                    tc_commit(&sh.o_full[1]);
-                }
+        // =============================================================== units and their rows
+        registers_down<kProductRegisters>();
+        constexpr uint32_t kLanes = kDim == 64 ? 8 : 16, kPerWarp = 32 / kLanes;   // lanes of a row (one 16-byte unit each), rows at a time
+        constexpr int kBatch = 8;                                                  // loads in flight
+        const uint32_t unit16 = lane & (kLanes - 1u), sub = lane / kLanes, loader = warp - 13u;
+        const bool in_row = unit16 < kDim / 8u;
+        uint32_t q_use = 0;
+        bool ok = true;
+        for (uint32_t un = 0; ok; ++un) {
+            PromptUnit unit;
+            walk.next(kv, batch, q, few_rows, unit);
+            if (loader == 0u) {
+                if (un >= 4u) ok = bar_wait(&sh.unit_free[un & 3u], (un >> 2 & 1u) ^ 1u, sh.dead);
+                if (!ok) break;
+                unit.ref = unit.there ? value_reference(kv, unit.slot, unit.span.piece(0) << (7u - kv.page_shift), unit.head) : 1.f;
+                if (lane == 0) sh.unit[un & 3u] = unit;
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.unit_full[un & 3u]);
             }
-            if (!ok) {               // given up: say so, and let the products that were issued end
-                atomicOr(&kv.head->status, kKvStatInternal);
-                sh.dead = 0;
-                tc_commit(&sh.drained);
-                bar_wait_one(&sh.drained, 0u, sh);
+            if (!unit.there) break;
+            for (uint32_t half = 0; ok && half < (unit.two ? 2u : 1u); ++half, ++q_use) {
+                const uint32_t buffer = q_use % 3u;
+                if (q_use >= 3u) ok = bar_wait(&sh.q_empty[buffer], (q_use / 3u & 1u) ^ 1u, sh.dead);
+                if (!ok) break;
+                unsigned char* tile = tiles + buffer * kTile + (unit16 >> 3) * kSlabBytes;
+                const uint32_t rows = (uint32_t)unit.rows * q.group, r0 = unit.tile * kPromptRows + half * 128u;
+                for (uint32_t base = loader * kPerWarp + sub; base < 128u; base += 3u * kPerWarp * kBatch) {
+                    uint4 v[kBatch];
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) {
+                        const uint32_t row = base + 3u * kPerWarp * i, r = r0 + row;
+                        v[i] = make_uint4(0u, 0u, 0u, 0u);
+                        if (row < 128u && r < rows && in_row)
+                            v[i] = __ldg((const uint4*)(q.q + (int64_t)(unit.row0 + (int)(r / q.group)) * q.q_row +
+                                                        (int64_t)(unit.head * q.group + r % q.group) * q.q_head) + unit16);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) {
+                        const uint32_t row = base + 3u * kPerWarp * i;
+                        if constexpr (!__is_same(T, __half)) {
+                            uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                            float top = 0.f;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float2 f = to_float2<T>(x[e]);
+                                top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+                            }
+#pragma unroll
+                            for (uint32_t d = 1; d < kLanes; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                            const int e2 = row_exponent(top);
+                            const float up = power_of_two(e2);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float2 f = to_float2<T>(x[e]);
+                                x[e] = from_float2<__half>(f.x * up, f.y * up);
+                            }
+                            v[i] = make_uint4(x[0], x[1], x[2], x[3]);
+                            if (unit16 == 0u && row < 128u) sh.factor[buffer][row] = power_of_two(-e2);
+                        }
+                        if (row < 128u && in_row) *(uint4*)(tile + row * 128u + ((unit16 & 7u) ^ (row & 7u)) * 16u) = v[i];
+                    }
+                }
+                proxy_fence();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.q_full[buffer]);
             }
         }
-        __syncwarp();
     }
     // every product has been waited for by the warps that read its result, or above
     __syncthreads();
     if (warp == 12u) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tmem));
     }
 }
 
