@@ -8,16 +8,14 @@
 //
 // One block of 512 threads per SM, warp-specialised around mbarriers; the launch's registers are shared
 // out again by role:
-//   warps 0 - 3, 4 - 7   softmax of rows 0 - 127 and 128 - 255, one thread per row: reads S from tensor
-//                        memory (twice, for the maximum and for the exponentials: a read costs about 200
-//                        cycles, holding 128 columns would cost the registers of the other roles), writes P
-//                        over it as fp16, rescales the output sum when its row's maximum has grown by more
-//                        than 2^8, writes results
+//   warps 0 - 3, 4 - 7   softmax of rows 0 - 127 and 128 - 255, one thread per row: reads S from tensor memory
+//                        64 columns at a time, writes P over them as fp16, rescales the output sum when its row's
+//                        maximum has grown by more than 2^15, writes results
 //   warps 8 - 11         bytes of the cache to fp16 in shared memory (keys and values, two pieces each);
 //                        a piece's bytes are requested while the piece before it is stored
 //   warp 12              issues tcgen05.mma:  S = Q K'^T (both in shared memory) and O += P V' (P in tensor
-//                        memory); order QK0(j), PV1(j-1), QK1(j), PV0(j) without regard to where units end,
-//                        so that one half's products run under the other half's softmax
+//                        memory); as soon as a half's P is complete its O += P V' and its next S follow each
+//                        other in the queue, and the other half's softmax runs meanwhile
 //   warps 13 - 15        walk along the share, publish each unit to the others, and bring its rows to shared
 //                        memory as fp16 (three tiles of 128 rows in turn, so one unit ahead)
 // Keys lie [token][dim] and are a K-major operand; values lie [token][dim] too, which is an MN-major
@@ -39,10 +37,12 @@ constexpr uint32_t kPromptUnitCost = 2;          // starting and ending a unit, 
 constexpr uint32_t kSlabBytes = 128 * 128;       // 128 rows of 64 fp16 numbers
 // Registers a thread of each role (the launch's 512 x 128 are shared out again).  None may spill: with the tiles
 // taking 227 KB little is left of the L1 cache, and a spilled register comes back from L2.
-constexpr int kSoftmaxRegisters = 144, kConvertRegisters = 128, kProductRegisters = 96;
+constexpr int kSoftmaxRegisters = 152, kConvertRegisters = 120, kProductRegisters = 88;
 static_assert(256 * kSoftmaxRegisters + 128 * kConvertRegisters + 128 * kProductRegisters <= 512 * 128, "no more than the launch has");
 constexpr uint32_t kWaitLimit = 1u << 20;        // tries of a barrier wait (each may suspend) before the kernel gives up
-constexpr float kGrowth = 8.f;                   // P stays below 2^8: the output sum is rescaled when the maximum grows by more
+// The output sum is rescaled only when a row's maximum has grown by more than 2^15: P then stays in fp16's range.  A
+// rescale waits for the product before and costs its half about 4000 cycles; at 2^8 every tenth piece had one.
+constexpr float kGrowth = 15.f;
 constexpr uint32_t kPromptArrived = 512;         // first counter of KvWorkHeader::arrived that is this kernel's
 
 template <int kDim>
@@ -194,6 +194,14 @@ __device__ __forceinline__ void hide_unseen(uint32_t (&s)[32], uint32_t seen)
     for (int e = 0; e < 32; ++e) s[e] = seen & (1u << e) ? s[e] : 0xff800000u;
 }
 
+// a load that leaves the L1 cache, what there is of it, to others
+__device__ __forceinline__ uint4 load_once(const uint4* p)
+{
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
 // Matrix descriptor of a tile stored as 128-byte rows with the 128-byte swizzle.  High word, the same for all tiles
 // here: 1024 bytes from one group of eight rows to the next (in 16-byte units), version 1, swizzle mode 2.  Low word:
 // address and leading offset, in 16-byte units.  Kept apart, so that the one thread that issues products works on
@@ -318,7 +326,7 @@ struct PromptWalk {
 };
 
 struct PromptShared {
-    uint64_t q_full[3], q_empty[3], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], scale_full[4];
+    uint64_t q_full[3], q_empty[3], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[4], o_full[4], scale_full[4];   // p_, o_full: half, part (64 tokens)
     uint64_t unit_full[4], unit_free[4];
     uint64_t joint[2], drained;                  // the warps of a half meet; products of a run that was given up
     PromptUnit unit[4];                          // ring of units
@@ -425,14 +433,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             bar_init(&sh.v_full[i], 4);
             bar_init(&sh.v_empty[i], 1);
             bar_init(&sh.s_full[i], 1);
-            bar_init(&sh.p_full[i], 4);
-            bar_init(&sh.o_full[i], 1);
             bar_init(&sh.joint[i], 4);
         }
         for (int i = 0; i < 4; ++i) {
             bar_init(&sh.scale_full[i], 4);
+            bar_init(&sh.p_full[i], 4);
+            bar_init(&sh.o_full[i], 1);
             bar_init(&sh.unit_full[i], 1);
-            bar_init(&sh.unit_free[i], 13);      // softmax, converting and product warps
+            bar_init(&sh.unit_free[i], 16);      // every warp
         }
         bar_init(&sh.drained, 1);
         sh.dead = 0;
@@ -453,7 +461,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         const uint32_t half = warp >> 2, row = threadIdx.x & 127u;
         const uint32_t lanes = (warp & 3u) << 21;            // lane field of a tensor memory address
         const uint32_t s_at = lanes + half * 128u, o_at = lanes + 256u + half * 128u;
-        uint32_t piece_count = 0, s_count = 0, unit_count = 0;   // pieces of the block, of this half, units of this half
+        uint32_t piece_count = 0, s_count = 0;                   // pieces of the block, of this half
         uint32_t q_use = 0;                                      // Q tiles used before the unit
         uint32_t joints = 0;                                     // times this half's warps have met
         auto meet = [&]() {
@@ -507,64 +515,58 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                     if (q.window) after = (int)max((int64_t)-1, min((int64_t)127, (int64_t)position - (int64_t)q.window - t0));
                     kept = (int)max((int64_t)0, min((int64_t)128, (int64_t)q.sinks - t0));
                 }
-                float top = -INFINITY;
 #pragma unroll 1
-                for (int c = 0; c < 4; c += 2) {
+                for (uint32_t part = 0; ok && part < 2u; ++part) {
                     uint32_t s[2][32];
-                    tm_load32(s_at + 32u * c, s[0]);
-                    tm_load32(s_at + 32u * c + 32u, s[1]);
+                    tm_load32(s_at + 64u * part, s[0]);
+                    tm_load32(s_at + 64u * part + 32u, s[1]);
                     tm_wait_load();
                     if (!whole) {
-                        hide_unseen(s[0], seen_bits(upto, after, kept, 32 * c));
-                        hide_unseen(s[1], seen_bits(upto, after, kept, 32 * c + 32));
+                        hide_unseen(s[0], seen_bits(upto, after, kept, 64 * part));
+                        hide_unseen(s[1], seen_bits(upto, after, kept, 64 * part + 32));
                     }
+                    float top = -INFINITY;
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
-                        const float2 sc = *(const float2*)&sh.scales[ring][2 * c + h];
+                        const float2 sc = *(const float2*)&sh.scales[ring][4 * part + h];
                         float best = __uint_as_float(s[h >> 1][16 * (h & 1)]);
 #pragma unroll
                         for (int e = 1; e < 16; ++e) best = fmaxf(best, __uint_as_float(s[h >> 1][16 * (h & 1) + e]));
                         // a factor of 0 times minus infinity would be NaN
                         top = fmaxf(top, best == -INFINITY ? -INFINITY : fmaf(best, sc.x * row_factor, sc.y));
                     }
-                }
-                // the maximum moves when it has grown by more than kGrowth, or from nothing
-                if (!(top > m + kGrowth || (m == -INFINITY && top > -INFINITY))) top = m;
-                if (__any_sync(0xffffffffu, top != m)) {
-                    const float shrink = top == m ? 1.f : ex2(m - top);
-                    l *= shrink;
-                    m = top;
-                    if (j > 0) {
-                        const uint64_t by = pair(shrink, shrink);
+                    // the maximum moves when it has grown by more than kGrowth, or from nothing
+                    if (!(top > m + kGrowth || (m == -INFINITY && top > -INFINITY))) top = m;
+                    if (__any_sync(0xffffffffu, top != m)) {
+                        const float shrink = top == m ? 1.f : ex2(m - top);
+                        l *= shrink;
+                        m = top;
+                        if (j > 0u || part > 0u) {
+                            // the product before, of part 0 of this piece or of part 1 of the last, has to be in the sum
+                            ok = bar_wait(&sh.o_full[2u * half + (part ^ 1u)], (s_count ^ part ^ 1u) & 1u, sh.dead);
+                            if (!ok) break;
+                            tc_fence_after();
+                            const uint64_t by = pair(shrink, shrink);
 #pragma unroll 1
-                        for (int c = 0; c < kDim / 16; ++c) {
-                            uint32_t o[16];
-                            tm_load16(o_at + 16u * c, o);
-                            tm_wait_load();
+                            for (int c = 0; c < kDim / 32; ++c) {
+                                uint32_t o[32];
+                                tm_load32(o_at + 32u * c, o);
+                                tm_wait_load();
 #pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                const float2 v = unpair(mul2(pair(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), by));
-                                o[e] = __float_as_uint(v.x);
-                                o[e + 1] = __float_as_uint(v.y);
+                                for (int e = 0; e < 32; e += 2) {
+                                    const float2 v = unpair(mul2(pair(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), by));
+                                    o[e] = __float_as_uint(v.x);
+                                    o[e + 1] = __float_as_uint(v.y);
+                                }
+                                tm_store32(o_at + 32u * c, o);
                             }
-                            tm_store16(o_at + 16u * c, o);
                         }
                     }
-                }
-                const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll 1
-                for (int c = 0; c < 4; c += 2) {
-                    uint32_t s[2][32], p[32];
-                    tm_load32(s_at + 32u * c, s[0]);
-                    tm_load32(s_at + 32u * c + 32u, s[1]);
-                    tm_wait_load();
-                    if (!whole) {
-                        hide_unseen(s[0], seen_bits(upto, after, kept, 32 * c));
-                        hide_unseen(s[1], seen_bits(upto, after, kept, 32 * c + 32));
-                    }
+                    const float base = m == -INFINITY ? 0.f : m;
+                    uint32_t p[32];
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
-                        const float4 sc = sh.scales[ring][2 * c + h];
+                        const float4 sc = sh.scales[ring][4 * part + h];
                         const float f = fmaxf(sc.x * row_factor, 1e-37f), add = sc.y - base;   // not 0, for the masked ones' sake
                         const uint64_t ff = pair(f, f), aa = pair(add, add);
                         uint64_t sum = 0ull;
@@ -579,18 +581,18 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                         const float2 both = unpair(sum);
                         l = fmaf(both.x + both.y, sc.z, l);
                     }
-                    tm_store32(s_at + 16u * c, p);      // over columns that have been read
+                    tm_store32(s_at + 32u * part, p);        // over columns that have been read
+                    tm_wait_store();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sh.p_full[2u * half + part]);
                 }
-                tm_wait_store();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(&sh.p_full[half]);
+                if (!ok) break;
             }
             if (!ok) break;
-            ok = bar_wait(&sh.o_full[half], unit_count & 1u, sh.dead);
+            ok = bar_wait(&sh.o_full[2u * half + 1u], (s_count & 1u) ^ 1u, sh.dead);
             if (!ok) break;
             tc_fence_after();
-            ++unit_count;
 
             // ---- results
             const bool complete = pieces == unit.span.count;
@@ -752,7 +754,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                                     (inside + 8u * (g & 1) + sub_row) * kDim + chunk * 16u;
 #pragma unroll
                 for (int h = 0; h < kHalves; ++h)
-                    to[g][h] = page >= 0 && (h == 0 || in_second) ? __ldg((const uint4*)(at + 64u * h))
+                    to[g][h] = page >= 0 && (h == 0 || in_second) ? load_once((const uint4*)(at + 64u * h))
                                                                   : make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
             }
         };
@@ -818,8 +820,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         registers_down<kProductRegisters>();
         constexpr uint32_t kQ = kWindow, kK = kWindow + 3u * kTile, kV = kWindow + 5u * kTile;
         const bool leader = elected();
-        auto scores = [&](uint32_t half, uint32_t q_buffer, uint32_t stage) {
-            const uint32_t a = (kQ >> 4 | 1u << 16) + q_buffer * (kTile >> 4), b = (kK >> 4 | 1u << 16) + stage * (kTile >> 4);
+        // S[half] = Q K'^T for a piece
+        auto scores = [&](uint32_t half, uint32_t a, uint32_t b) {
             if (leader) {
 #pragma unroll
                 for (uint32_t k = 0; k < kDim / 16; ++k) {
@@ -830,13 +832,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             }
             __syncwarp();
         };
-        auto outputs = [&](uint32_t half, uint32_t stage, bool add) {
-            const uint32_t b = (kV >> 4 | (kSlabBytes >> 4) << 16) + stage * (kTile >> 4);
+        // O[half] += P V' for 64 tokens of a piece
+        auto outputs = [&](uint32_t half, uint32_t part, uint32_t b, bool add) {
             if (leader) {
 #pragma unroll
-                for (uint32_t k = 0; k < 8u; ++k)
-                    tc_product_tensor(256u + half * 128u, half * 128u + 8u * k, b + (2048u >> 4) * k, product_descriptor(kDim, true),
-                                      k > 0u || add);
+                for (uint32_t k = 0; k < 4u; ++k)
+                    tc_product_tensor(256u + half * 128u, half * 128u + part * 32u + 8u * k, b + (8192u >> 4) * part + (2048u >> 4) * k,
+                                      product_descriptor(kDim, true), k > 0u || add);
+                tc_commit(&sh.o_full[2u * half + part]);
             }
             __syncwarp();
         };
@@ -844,56 +847,62 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             if (leader) tc_commit(b);
             __syncwarp();
         };
-        uint32_t count = 0, p_use[2] = {0u, 0u}, q_use = 0;
-        bool pending = false, pending_add = false, pending_last = false;     // half 1's second product of the piece before
+        // Turn c issues the scores of piece c and the outputs of piece c - 1 (of the same unit or the one before).
+        uint32_t count = 0, q_use = 0, uses[2] = {0u, 0u};       // pieces; Q tiles; outputs' pieces of each half
+        bool had = false, had_two = false, had_add = false;      // piece c - 1: is there, has a half 1, is not its unit's first
         bool ok = true;
         for (uint32_t un = 0; ok; ++un) {
             ok = bar_wait(&sh.unit_full[un & 3u], un >> 2 & 1u, sh.dead);
             if (!ok) break;
             const PromptUnit& unit = sh.unit[un & 3u];
-            const uint32_t there = __shfl_sync(0xffffffffu, unit.there, 0), two = __shfl_sync(0xffffffffu, unit.two, 0);
-            // after the last unit one more turn issues what is pending
-            const uint32_t pieces = there ? __shfl_sync(0xffffffffu, unit.to - unit.from, 0) : pending ? 1u : 0u;
+            const bool there = __shfl_sync(0xffffffffu, unit.there, 0), two = there && __shfl_sync(0xffffffffu, unit.two, 0);
+            // behind the last unit one more turn for the last piece's outputs
+            const uint32_t pieces = there ? __shfl_sync(0xffffffffu, unit.to - unit.from, 0) : had ? 1u : 0u;
             __syncwarp();
             if (lane == 0) bar_arrive(&sh.unit_free[un & 3u]);
-            const uint32_t use = q_use;
+            const uint32_t tile[2] = {q_use % 3u, (q_use + 1u) % 3u}, tile_parity[2] = {q_use / 3u & 1u, (q_use + 1u) / 3u & 1u};
             q_use += two ? 2u : 1u;
             for (uint32_t j = 0; ok && j < pieces; ++j) {
                 const uint32_t stage = count & 1u, parity = count >> 1 & 1u;
-                const bool last = j + 1u == pieces;
-                if (there) ok = bar_wait(&sh.k_full[stage], parity, sh.dead);
-                // QK0, PV1 of the piece before, QK1, PV0
-#pragma unroll 1
-                for (uint32_t half = 0; ok && half < 2u; ++half) {
-                    if (there && (half == 0u || two)) {
-                        const uint32_t q_now = use + half;
-                        if (j == 0u) {
-                            ok = bar_wait(&sh.q_full[q_now % 3u], q_now / 3u & 1u, sh.dead);
-                            if (!ok) break;
+                const uint32_t k_low = (kK >> 4 | 1u << 16) + stage * (kTile >> 4);
+                const uint32_t v_low = (kV >> 4 | (kSlabBytes >> 4) << 16) + (stage ^ 1u) * (kTile >> 4);
+                if (had) ok = bar_wait(&sh.v_full[stage ^ 1u], (count - 1u) >> 1 & 1u, sh.dead);
+                if (ok && there) ok = bar_wait(&sh.k_full[stage], parity, sh.dead);
+#pragma unroll
+                for (uint32_t half = 0; half < 2u; ++half) {
+#pragma unroll
+                    for (uint32_t part = 0; part < 2u; ++part)
+                        if (ok && had && (half == 0u || had_two)) {
+                            ok = bar_wait(&sh.p_full[2u * half + part], uses[half] & 1u, sh.dead);
+                            if (ok) {
+                                tc_fence_after();
+                                outputs(half, part, v_low, had_add || part > 0u);
+                            }
                         }
-                        tc_fence_after();
-                        scores(half, q_now % 3u, stage);
-                        if (last) commit(&sh.q_empty[q_now % 3u]);
+                    if (ok && there && (half == 0u || two)) {
+                        if (j == 0u) ok = bar_wait(&sh.q_full[tile[half]], tile_parity[half], sh.dead);
+                        if (ok) {
+                            tc_fence_after();
+                            scores(half, (kQ >> 4 | 1u << 16) + tile[half] * (kTile >> 4), k_low);
+                        }
                     }
-                    if (half == 1u && there) commit(&sh.k_empty[stage]);
-                    if (half ? there != 0u : pending) {
-                        const uint32_t of = half ^ 1u, v_stage = half ? stage : stage ^ 1u;
-                        const bool ends = half ? last : pending_last;
-                        ok = (!half || bar_wait(&sh.v_full[stage], parity, sh.dead)) && bar_wait(&sh.p_full[of], p_use[of]++ & 1u, sh.dead);
-                        if (!ok) break;
-                        tc_fence_after();
-                        outputs(of, v_stage, half ? j > 0u : pending_add);
-                        if (of == 1u || !two) commit(&sh.v_empty[v_stage]);
-                        if (ends) commit(&sh.o_full[of]);
-                    }
-                    if (half == 0u) pending = false;
                 }
-                if (there && two) {
-                    pending = true;
-                    pending_add = j > 0u;
-                    pending_last = last;
+                if (!ok) break;
+                if (had) {
+                    commit(&sh.v_empty[stage ^ 1u]);
+                    ++uses[0];
+                    uses[1] += had_two;
                 }
-                if (there) ++count;
+                had = there;
+                if (!there) break;
+                commit(&sh.k_empty[stage]);
+                if (j + 1u == pieces) {
+                    commit(&sh.q_empty[tile[0]]);
+                    if (two) commit(&sh.q_empty[tile[1]]);
+                }
+                had_two = two;
+                had_add = j > 0u;
+                ++count;
             }
             if (!there) break;
         }
@@ -907,22 +916,24 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         // =============================================================== units and their rows
         registers_down<kProductRegisters>();
         constexpr uint32_t kLanes = kDim == 64 ? 8 : 16, kPerWarp = 32 / kLanes;   // lanes of a row (one 16-byte unit each), rows at a time
-        constexpr int kBatch = 8;                                                  // loads in flight
         const uint32_t unit16 = lane & (kLanes - 1u), sub = lane / kLanes, loader = warp - 13u;
         const bool in_row = unit16 < kDim / 8u;
         uint32_t q_use = 0;
         bool ok = true;
         for (uint32_t un = 0; ok; ++un) {
-            PromptUnit unit;
-            walk.next(kv, batch, q, few_rows, unit);
-            if (loader == 0u) {
+            if (loader == 0u) {      // walk on, publish
                 if (un >= 4u) ok = bar_wait(&sh.unit_free[un & 3u], (un >> 2 & 1u) ^ 1u, sh.dead);
                 if (!ok) break;
-                unit.ref = unit.there ? value_reference(kv, unit.slot, unit.span.piece(0) << (7u - kv.page_shift), unit.head) : 1.f;
-                if (lane == 0) sh.unit[un & 3u] = unit;
+                PromptUnit u;
+                walk.next(kv, batch, q, few_rows, u);
+                u.ref = u.there ? value_reference(kv, u.slot, u.span.piece(0) << (7u - kv.page_shift), u.head) : 1.f;
+                if (lane == 0) sh.unit[un & 3u] = u;
                 __syncwarp();
                 if (lane == 0) bar_arrive(&sh.unit_full[un & 3u]);
             }
+            ok = bar_wait(&sh.unit_full[un & 3u], un >> 2 & 1u, sh.dead);
+            if (!ok) break;
+            const PromptUnit& unit = sh.unit[un & 3u];
             if (!unit.there) break;
             for (uint32_t half = 0; ok && half < (unit.two ? 2u : 1u); ++half, ++q_use) {
                 const uint32_t buffer = q_use % 3u;
@@ -930,46 +941,55 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 if (!ok) break;
                 unsigned char* tile = tiles + buffer * kTile + (unit16 >> 3) * kSlabBytes;
                 const uint32_t rows = (uint32_t)unit.rows * q.group, r0 = unit.tile * kPromptRows + half * 128u;
-                for (uint32_t base = loader * kPerWarp + sub; base < 128u; base += 3u * kPerWarp * kBatch) {
-                    uint4 v[kBatch];
+                // all of the tile's copies in flight at once
+                for (uint32_t row = loader * kPerWarp + sub; row < 128u; row += 3u * kPerWarp) {
+                    const uint32_t r = r0 + row;
+                    unsigned char* to = tile + row * 128u + ((unit16 & 7u) ^ (row & 7u)) * 16u;
+                    if (!in_row) continue;
+                    if (r < rows)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(shared_address(to)),
+                                     "l"((const uint4*)(q.q + (int64_t)(unit.row0 + (int)(r / q.group)) * q.q_row +
+                                                        (int64_t)(unit.head * q.group + r % q.group) * q.q_head) + unit16)
+                                     : "memory");
+                    else
+                        *(uint4*)to = make_uint4(0u, 0u, 0u, 0u);
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                __syncwarp();
+                if constexpr (!__is_same(T, __half)) {
+                    // bf16 to fp16 in place, a power of two taken out of each row
+#pragma unroll 4
+                    for (uint32_t base = loader * kPerWarp; base < 128u; base += 3u * kPerWarp) {
+                        const uint32_t row = base + sub;
+                        unsigned char* to = tile + row * 128u + ((unit16 & 7u) ^ (row & 7u)) * 16u;
+                        const bool mine = in_row && row < 128u;
+                        const uint4 v = mine ? *(uint4*)to : make_uint4(0u, 0u, 0u, 0u);
+                        uint32_t x[4] = {v.x, v.y, v.z, v.w};
+                        float top = 0.f;
 #pragma unroll
-                    for (int i = 0; i < kBatch; ++i) {
-                        const uint32_t row = base + 3u * kPerWarp * i, r = r0 + row;
-                        v[i] = make_uint4(0u, 0u, 0u, 0u);
-                        if (row < 128u && r < rows && in_row)
-                            v[i] = __ldg((const uint4*)(q.q + (int64_t)(unit.row0 + (int)(r / q.group)) * q.q_row +
-                                                        (int64_t)(unit.head * q.group + r % q.group) * q.q_head) + unit16);
-                    }
-#pragma unroll
-                    for (int i = 0; i < kBatch; ++i) {
-                        const uint32_t row = base + 3u * kPerWarp * i;
-                        if constexpr (!__is_same(T, __half)) {
-                            uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                            float top = 0.f;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float2 f = to_float2<T>(x[e]);
-                                top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
-                            }
-#pragma unroll
-                            for (uint32_t d = 1; d < kLanes; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                            const int e2 = row_exponent(top);
-                            const float up = power_of_two(e2);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float2 f = to_float2<T>(x[e]);
-                                x[e] = from_float2<__half>(f.x * up, f.y * up);
-                            }
-                            v[i] = make_uint4(x[0], x[1], x[2], x[3]);
-                            if (unit16 == 0u && row < 128u) sh.factor[buffer][row] = power_of_two(-e2);
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 f = to_float2<T>(x[e]);
+                            top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
                         }
-                        if (row < 128u && in_row) *(uint4*)(tile + row * 128u + ((unit16 & 7u) ^ (row & 7u)) * 16u) = v[i];
+#pragma unroll
+                        for (uint32_t d = 1; d < kLanes; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                        const int e2 = row_exponent(top);
+                        const float up = power_of_two(e2);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 f = to_float2<T>(x[e]);
+                            x[e] = from_float2<__half>(f.x * up, f.y * up);
+                        }
+                        if (mine) *(uint4*)to = make_uint4(x[0], x[1], x[2], x[3]);
+                        if (unit16 == 0u && row < 128u) sh.factor[buffer][row] = power_of_two(-e2);
                     }
                 }
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) bar_arrive(&sh.q_full[buffer]);
             }
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sh.unit_free[un & 3u]);
         }
     }
     // every product has been waited for by the warps that read its result, or above
