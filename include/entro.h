@@ -464,7 +464,7 @@ typedef struct {
     void *out_dev;                 /* the same shape and type, strides of its own; must not overlap q */
     float *lse_dev;                /* [rows][q_heads] natural log of the softmax sum, or NULL */
     int64_t q_row_stride, q_head_stride, out_row_stride, out_head_stride;
-    uint32_t q_heads;              /* a multiple of kv_heads; query head h reads kv head h / (q_heads / kv_heads) */
+    uint32_t q_heads;              /* a multiple of kv_heads, at most 16384; query head h reads kv head h / (q_heads / kv_heads) */
     uint32_t max_rows;             /* no sequence of the batch has more rows (0: not known) */
     uint32_t window;               /* 0: none */
     uint32_t sinks;

@@ -60,7 +60,7 @@ extern "C" entro_status entro_kv_attention(const entro_kv_cache* cache, const en
     if (a->type != ENTRO_FLOAT16 && a->type != ENTRO_BFLOAT16) return ENTRO_ERR_INVALID_ARG;
     if (!kv_strides_ok(a->q_row_stride, a->q_head_stride) || !kv_strides_ok(a->out_row_stride, a->out_head_stride))
         return ENTRO_ERR_INVALID_ARG;
-    if (a->q_heads == 0 || a->q_heads % kv.heads || a->q_heads > 65536u) return ENTRO_ERR_INVALID_ARG;
+    if (a->q_heads == 0 || a->q_heads % kv.heads || a->q_heads > kMostQueryHeads) return ENTRO_ERR_INVALID_ARG;
     if (!(a->softmax_scale >= 0.f && a->softmax_scale <= 3.4e38f)) return ENTRO_ERR_INVALID_ARG;
     Query q;
     q.q = (const unsigned char*)a->q_dev;
@@ -72,6 +72,7 @@ extern "C" entro_status entro_kv_attention(const entro_kv_cache* cache, const en
     q.out_head = 2 * a->out_head_stride;
     q.heads = a->q_heads;
     q.group = a->q_heads / kv.heads;
+    q.group_inverse = q.group == 1u ? 0u : 0xffffffffu / q.group + 1u;
     q.window = a->window;
     q.sinks = a->sinks;
     q.scale = a->softmax_scale > 0.f ? a->softmax_scale : 1.f / sqrtf((float)kv.dim);

@@ -24,8 +24,12 @@ struct Query {
     float* lse;
     int64_t q_row, q_head, out_row, out_head;    // strides in bytes
     uint32_t heads, group, window, sinks;
+    uint32_t group_inverse;                      // ceil(2^32 / group); 0 for a group of 1
     float scale;
+    // x / group for x below group + 2^16: x times the rounding of the inverse stays below 2^32
+    __device__ __forceinline__ uint32_t by_group(uint32_t x) const { return group_inverse ? __umulhi(x, group_inverse) : x; }
 };
+constexpr uint32_t kMostQueryHeads = 16384;
 
 namespace {
 

@@ -12,7 +12,7 @@
 //                        64 columns at a time, writes P over them as fp16, rescales the output sum when its row's
 //                        maximum has grown by more than 2^15, writes results
 //   warps 8 - 11         bytes of the cache to fp16 in shared memory (keys and values, two pieces each);
-//                        a piece's bytes are requested while the piece before it is stored
+//                        a tile's bytes are requested as soon as the tile before it is stored
 //   warp 12              issues tcgen05.mma:  S = Q K'^T (both in shared memory) and O += P V' (P in tensor
 //                        memory); as soon as a half's P is complete its O += P V' and its next S follow each
 //                        other in the queue, and the other half's softmax runs meanwhile
@@ -172,13 +172,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 __device__ __forceinline__ void tm_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -344,7 +337,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
     constexpr uint32_t kTile = kPromptSlabs<kDim> * kSlabBytes;
     extern __shared__ __align__(1024) unsigned char tiles[];
     unsigned char* const k_tile = tiles + 3 * kTile;         // [2] stages; the three Q tiles come first
-    unsigned char* const v_tile = tiles + 5 * kTile;         // [2] stages
+    // then two stages of value tiles
     PromptShared& sh = *(PromptShared*)(tiles + 7 * kTile);
     uint32_t* const seq_weight = sh.seq_weight;
     const uint32_t lane = threadIdx.x & 31u, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
@@ -546,19 +539,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                             ok = bar_wait(&sh.o_full[2u * half + (part ^ 1u)], (s_count ^ part ^ 1u) & 1u, sh.dead);
                             if (!ok) break;
                             tc_fence_after();
-                            const uint64_t by = pair(shrink, shrink);
 #pragma unroll 1
-                            for (int c = 0; c < kDim / 32; ++c) {
-                                uint32_t o[32];
-                                tm_load32(o_at + 32u * c, o);
+                            for (int c = 0; c < kDim / 16; ++c) {
+                                uint32_t o[16];
+                                tm_load16(o_at + 16u * c, o);
                                 tm_wait_load();
 #pragma unroll
-                                for (int e = 0; e < 32; e += 2) {
-                                    const float2 v = unpair(mul2(pair(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), by));
-                                    o[e] = __float_as_uint(v.x);
-                                    o[e + 1] = __float_as_uint(v.y);
-                                }
-                                tm_store32(o_at + 32u * c, o);
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+                                tm_store16(o_at + 16u * c, o);
                             }
                         }
                     }
@@ -702,7 +690,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         const uint32_t chunk = (lane & 1u) | (lane >> 4) << 1;
         constexpr int kHalves = kDim == 64 ? 1 : 2;                              // 64-byte parts of a cache row
         const bool in_second = kDim != 96 || chunk < 2u;
-        // a piece whose pages have been looked up: two ahead of the piece that is stored, one ahead of its loads
+        // a piece whose pages have been looked up
         struct Place {
             int page[2];             // of the warp's two groups of 16 tokens
             uint32_t inside, head;   // first token's place in its page (the second's is 16 further, in the same or the next page)
@@ -783,37 +771,34 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             proxy_fence();
             __syncwarp();
         };
-        uint4 kb[4][kHalves], vb[4][kHalves];
-        Place now, next = look_up();
-        now.there = false;           // the first turn only requests
-        for (uint32_t count = 0; next.there || now.there;) {
-            const uint32_t stage = count & 1u, parity = (count >> 1 & 1u) ^ 1u;
-            if (now.there) {
-                if (!bar_wait(&sh.k_empty[stage], parity, sh.dead)) break;
-                if (lane < 2u) {
-                    // the scales of a piece four places back are no longer read: its S tiles have been followed by newer ones
-                    const float rel = relative_scale(value_scale, now.by_ref);
-                    sh.scales[count & 3u][2u * w + lane] = (lane ? now.page[1] : now.page[0]) >= 0
-                                                               ? make_float4(key_scale, lg2(rel), rcp(rel), 0.f)
-                                                               : make_float4(0.f, -INFINITY, 0.f, 0.f);
-                }
-                store(kb, k_tile + stage * kTile);
-                if (lane == 0) {
-                    bar_arrive(&sh.scale_full[count & 3u]);
-                    bar_arrive(&sh.k_full[stage]);
-                }
+        // keys of piece 0, values of piece 0, keys of piece 1, ...: a tile is requested as soon as the one before is stored
+        uint4 buffer[4][kHalves];
+        Place now = look_up(), next = now;
+        if (now.there) {
+            load(buffer, now, 0u);
+            load_scales(now);
+        }
+        for (uint32_t t = 0; now.there; ++t) {
+            const uint32_t which = t & 1u, count = t >> 1, stage = count & 1u, parity = (count >> 1 & 1u) ^ 1u;
+            if (!bar_wait(which ? &sh.v_empty[stage] : &sh.k_empty[stage], parity, sh.dead)) break;
+            if (which == 0u && lane < 2u) {
+                // the scales of a piece four places back are no longer read: its S tiles have been followed by newer ones
+                const float rel = relative_scale(value_scale, now.by_ref);
+                sh.scales[count & 3u][2u * w + lane] = (lane ? now.page[1] : now.page[0]) >= 0
+                                                           ? make_float4(key_scale, lg2(rel), rcp(rel), 0.f)
+                                                           : make_float4(0.f, -INFINITY, 0.f, 0.f);
             }
-            load(kb, next, 0u);
-            load_scales(next);
-            if (now.there) {
-                if (!bar_wait(&sh.v_empty[stage], parity, sh.dead)) break;
-                store(vb, v_tile + stage * kTile);
-                if (lane == 0) bar_arrive(&sh.v_full[stage]);
-                ++count;
+            store(buffer, k_tile + (2u * which + stage) * kTile);        // the value tiles lie behind the key tiles
+            if (lane == 0) {
+                if (which == 0u) bar_arrive(&sh.scale_full[count & 3u]);
+                bar_arrive(which ? &sh.v_full[stage] : &sh.k_full[stage]);
             }
-            load(vb, next, 1u);
-            now = next;
-            next = look_up();
+            if (which == 0u)
+                next = look_up();
+            else
+                now = next;
+            load(buffer, now, which ^ 1u);
+            if (which) load_scales(now);
         }
     } else if (warp == 12u) {
         // =============================================================== products
@@ -848,7 +833,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             __syncwarp();
         };
         // Turn c issues the scores of piece c and the outputs of piece c - 1 (of the same unit or the one before).
-        uint32_t count = 0, q_use = 0, uses[2] = {0u, 0u};       // pieces; Q tiles; outputs' pieces of each half
+        uint32_t count = 0, q_use = 0, uses = 0;                 // pieces; Q tiles; bit h: parity of half h's next outputs
         bool had = false, had_two = false, had_add = false;      // piece c - 1: is there, has a half 1, is not its unit's first
         bool ok = true;
         for (uint32_t un = 0; ok; ++un) {
@@ -860,7 +845,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             const uint32_t pieces = there ? __shfl_sync(0xffffffffu, unit.to - unit.from, 0) : had ? 1u : 0u;
             __syncwarp();
             if (lane == 0) bar_arrive(&sh.unit_free[un & 3u]);
-            const uint32_t tile[2] = {q_use % 3u, (q_use + 1u) % 3u}, tile_parity[2] = {q_use / 3u & 1u, (q_use + 1u) / 3u & 1u};
+            const uint32_t tile0 = q_use;
             q_use += two ? 2u : 1u;
             for (uint32_t j = 0; ok && j < pieces; ++j) {
                 const uint32_t stage = count & 1u, parity = count >> 1 & 1u;
@@ -868,37 +853,37 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 const uint32_t v_low = (kV >> 4 | (kSlabBytes >> 4) << 16) + (stage ^ 1u) * (kTile >> 4);
                 if (had) ok = bar_wait(&sh.v_full[stage ^ 1u], (count - 1u) >> 1 & 1u, sh.dead);
                 if (ok && there) ok = bar_wait(&sh.k_full[stage], parity, sh.dead);
-#pragma unroll
+#pragma unroll 1
                 for (uint32_t half = 0; half < 2u; ++half) {
-#pragma unroll
+#pragma unroll 1
                     for (uint32_t part = 0; part < 2u; ++part)
                         if (ok && had && (half == 0u || had_two)) {
-                            ok = bar_wait(&sh.p_full[2u * half + part], uses[half] & 1u, sh.dead);
+                            ok = bar_wait(&sh.p_full[2u * half + part], uses >> half & 1u, sh.dead);
                             if (ok) {
                                 tc_fence_after();
                                 outputs(half, part, v_low, had_add || part > 0u);
                             }
                         }
                     if (ok && there && (half == 0u || two)) {
-                        if (j == 0u) ok = bar_wait(&sh.q_full[tile[half]], tile_parity[half], sh.dead);
+                        const uint32_t tile = (tile0 + half) % 3u;
+                        if (j == 0u) ok = bar_wait(&sh.q_full[tile], (tile0 + half) / 3u & 1u, sh.dead);
                         if (ok) {
                             tc_fence_after();
-                            scores(half, (kQ >> 4 | 1u << 16) + tile[half] * (kTile >> 4), k_low);
+                            scores(half, (kQ >> 4 | 1u << 16) + tile * (kTile >> 4), k_low);
                         }
                     }
                 }
                 if (!ok) break;
                 if (had) {
                     commit(&sh.v_empty[stage ^ 1u]);
-                    ++uses[0];
-                    uses[1] += had_two;
+                    uses ^= had_two ? 3u : 1u;
                 }
                 had = there;
                 if (!there) break;
                 commit(&sh.k_empty[stage]);
                 if (j + 1u == pieces) {
-                    commit(&sh.q_empty[tile[0]]);
-                    if (two) commit(&sh.q_empty[tile[1]]);
+                    commit(&sh.q_empty[tile0 % 3u]);
+                    if (two) commit(&sh.q_empty[(tile0 + 1u) % 3u]);
                 }
                 had_two = two;
                 had_add = j > 0u;
@@ -941,15 +926,16 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 if (!ok) break;
                 unsigned char* tile = tiles + buffer * kTile + (unit16 >> 3) * kSlabBytes;
                 const uint32_t rows = (uint32_t)unit.rows * q.group, r0 = unit.tile * kPromptRows + half * 128u;
+                const uint32_t token0 = r0 / q.group, head0 = r0 - token0 * q.group;
+                const unsigned char* from = q.q + (int64_t)(unit.row0 + (int)token0) * q.q_row + (int64_t)(unit.head * q.group) * q.q_head;
                 // all of the tile's copies in flight at once
                 for (uint32_t row = loader * kPerWarp + sub; row < 128u; row += 3u * kPerWarp) {
-                    const uint32_t r = r0 + row;
+                    const uint32_t r = r0 + row, token = q.by_group(head0 + row), h = head0 + row - token * q.group;
                     unsigned char* to = tile + row * 128u + ((unit16 & 7u) ^ (row & 7u)) * 16u;
                     if (!in_row) continue;
                     if (r < rows)
                         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(shared_address(to)),
-                                     "l"((const uint4*)(q.q + (int64_t)(unit.row0 + (int)(r / q.group)) * q.q_row +
-                                                        (int64_t)(unit.head * q.group + r % q.group) * q.q_head) + unit16)
+                                     "l"((const uint4*)(from + (int64_t)token * q.q_row + (int64_t)h * q.q_head) + unit16)
                                      : "memory");
                     else
                         *(uint4*)to = make_uint4(0u, 0u, 0u, 0u);
