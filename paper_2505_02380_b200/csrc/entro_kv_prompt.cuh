@@ -9,8 +9,8 @@
 // One block of 512 threads per SM, warp-specialised around mbarriers; the launch's registers are shared
 // out again by role:
 //   warps 0 - 3, 4 - 7   softmax of rows 0 - 127 and 128 - 255, one thread per row: reads S from tensor memory
-//                        64 columns at a time, writes P over them as fp16, rescales the output sum when its row's
-//                        maximum has grown by more than 2^15, writes results
+//                        64 columns at a time, writes P over them as fp16, moves its row's maximum (and
+//                        rescales the output sum) when P would leave fp16's range, writes results
 //   warps 8 - 11         bytes of the cache to fp16 in shared memory (keys and values, two pieces each);
 //                        a tile's bytes are requested as soon as the tile before it is stored
 //   warp 12              issues tcgen05.mma:  S = Q K'^T (both in shared memory) and O += P V' (P in tensor
@@ -33,16 +33,18 @@ constexpr uint32_t kPromptThreads = 512;
 constexpr uint32_t kPromptRows = 256;            // rows of a unit
 constexpr uint32_t kPromptBlocks = 160;          // most blocks of a launch
 constexpr uint32_t kPromptMinPieces = 2;         // a share is not made smaller than this
-constexpr uint32_t kPromptUnitCost = 2;          // starting and ending a unit, in pieces
+constexpr uint32_t kPromptUnitCost = 4;          // starting and ending a unit, in pieces
 constexpr uint32_t kSlabBytes = 128 * 128;       // 128 rows of 64 fp16 numbers
 // Registers a thread of each role (the launch's 512 x 128 are shared out again).  None may spill: with the tiles
 // taking 227 KB little is left of the L1 cache, and a spilled register comes back from L2.
-constexpr int kSoftmaxRegisters = 152, kConvertRegisters = 120, kProductRegisters = 88;
+constexpr int kSoftmaxRegisters = 176, kConvertRegisters = 80, kProductRegisters = 80;
 static_assert(256 * kSoftmaxRegisters + 128 * kConvertRegisters + 128 * kProductRegisters <= 512 * 128, "no more than the launch has");
 constexpr uint32_t kWaitLimit = 1u << 20;        // tries of a barrier wait (each may suspend) before the kernel gives up
-// The output sum is rescaled only when a row's maximum has grown by more than 2^15: P then stays in fp16's range.  A
-// rescale waits for the product before and costs its half about 4000 cycles; at 2^8 every tenth piece had one.
-constexpr float kGrowth = 15.f;
+// A row's maximum is moved only when it has to be: P (at most the sum of 16 columns) may reach 2^15 in fp16.  A move
+// waits for the product before and costs its half about 4000 cycles (at a growth of 2^8 every tenth piece had one), and
+// looking for the maximum at every piece costs a quarter of the softmax's instructions.  Once a sum has passed 2^15 the
+// maximum has grown by at least 2^11, so that the look that follows moves it.
+constexpr float kMostSum = 32768.f, kGrowth = 8.f;
 constexpr uint32_t kPromptArrived = 512;         // first counter of KvWorkHeader::arrived that is this kernel's
 
 template <int kDim>
@@ -510,65 +512,78 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 }
 #pragma unroll 1
                 for (uint32_t part = 0; ok && part < 2u; ++part) {
-                    uint32_t s[2][32];
-                    tm_load32(s_at + 64u * part, s[0]);
-                    tm_load32(s_at + 64u * part + 32u, s[1]);
-                    tm_wait_load();
-                    if (!whole) {
-                        hide_unseen(s[0], seen_bits(upto, after, kept, 64 * part));
-                        hide_unseen(s[1], seen_bits(upto, after, kept, 64 * part + 32));
-                    }
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        const float2 sc = *(const float2*)&sh.scales[ring][4 * part + h];
-                        float best = __uint_as_float(s[h >> 1][16 * (h & 1)]);
-#pragma unroll
-                        for (int e = 1; e < 16; ++e) best = fmaxf(best, __uint_as_float(s[h >> 1][16 * (h & 1) + e]));
-                        // a factor of 0 times minus infinity would be NaN
-                        top = fmaxf(top, best == -INFINITY ? -INFINITY : fmaf(best, sc.x * row_factor, sc.y));
-                    }
-                    // the maximum moves when it has grown by more than kGrowth, or from nothing
-                    if (!(top > m + kGrowth || (m == -INFINITY && top > -INFINITY))) top = m;
-                    if (__any_sync(0xffffffffu, top != m)) {
-                        const float shrink = top == m ? 1.f : ex2(m - top);
-                        l *= shrink;
-                        m = top;
-                        if (j > 0u || part > 0u) {
-                            // the product before, of part 0 of this piece or of part 1 of the last, has to be in the sum
-                            ok = bar_wait(&sh.o_full[2u * half + (part ^ 1u)], (s_count ^ part ^ 1u) & 1u, sh.dead);
-                            if (!ok) break;
-                            tc_fence_after();
+                    // P relative to the maximum as it is known.  Whether that still does is seen from the sums: only when one
+                    // passes kMostSum (or nothing was seen before) the maximum is looked for, and P made again.
+                    uint32_t p[32];
+                    float sums[4];
+                    bool look = __any_sync(0xffffffffu, m == -INFINITY);
 #pragma unroll 1
-                            for (int c = 0; c < kDim / 16; ++c) {
-                                uint32_t o[16];
-                                tm_load16(o_at + 16u * c, o);
-                                tm_wait_load();
+                    for (;;) {
+                        uint32_t s[2][32];
+                        tm_load32(s_at + 64u * part, s[0]);
+                        tm_load32(s_at + 64u * part + 32u, s[1]);
+                        tm_wait_load();
+                        if (!whole) {
+                            hide_unseen(s[0], seen_bits(upto, after, kept, 64 * part));
+                            hide_unseen(s[1], seen_bits(upto, after, kept, 64 * part + 32));
+                        }
+                        if (look) {
+                            float top = -INFINITY;
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
-                                tm_store16(o_at + 16u * c, o);
+                            for (int h = 0; h < 4; ++h) {
+                                const float2 sc = *(const float2*)&sh.scales[ring][4 * part + h];
+                                float best = __uint_as_float(s[h >> 1][16 * (h & 1)]);
+#pragma unroll
+                                for (int e = 1; e < 16; ++e) best = fmaxf(best, __uint_as_float(s[h >> 1][16 * (h & 1) + e]));
+                                top = fmaxf(top, fmaf(best, fmaxf(sc.x * row_factor, 1e-37f), sc.y));
+                            }
+                            if (!(top > m + kGrowth || (m == -INFINITY && top > -INFINITY))) top = m;
+                            if (__any_sync(0xffffffffu, top != m)) {
+                                const float shrink = top == m ? 1.f : ex2(m - top);
+                                l *= shrink;
+                                m = top;
+                                if (j > 0u || part > 0u) {
+                                    // the product before, of part 0 of this piece or of part 1 of the last, has to be in the sum
+                                    ok = bar_wait(&sh.o_full[2u * half + (part ^ 1u)], (s_count ^ part ^ 1u) & 1u, sh.dead);
+                                    if (!ok) break;
+                                    tc_fence_after();
+#pragma unroll 1
+                                    for (int c = 0; c < kDim / 16; ++c) {
+                                        uint32_t o[16];
+                                        tm_load16(o_at + 16u * c, o);
+                                        tm_wait_load();
+#pragma unroll
+                                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+                                        tm_store16(o_at + 16u * c, o);
+                                    }
+                                }
                             }
                         }
-                    }
-                    const float base = m == -INFINITY ? 0.f : m;
-                    uint32_t p[32];
+                        const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        const float4 sc = sh.scales[ring][4 * part + h];
-                        const float f = fmaxf(sc.x * row_factor, 1e-37f), add = sc.y - base;   // not 0, for the masked ones' sake
-                        const uint64_t ff = pair(f, f), aa = pair(add, add);
-                        uint64_t sum = 0ull;
+                        for (int h = 0; h < 4; ++h) {
+                            const float2 sc = *(const float2*)&sh.scales[ring][4 * part + h];
+                            // not 0: a factor of 0 times the minus infinity of a hidden column would be NaN
+                            const float f = fmaxf(sc.x * row_factor, 1e-37f), add = sc.y - base;
+                            const uint64_t ff = pair(f, f), aa = pair(add, add);
+                            uint64_t sum = 0ull;
 #pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
-                            const int at = 16 * (h & 1) + e;
-                            const float2 t = unpair(fma2(pair(__uint_as_float(s[h >> 1][at]), __uint_as_float(s[h >> 1][at + 1])), ff, aa));
-                            const float a = ex2(t.x), b = ex2(t.y);
-                            sum = add2(sum, pair(a, b));
-                            p[8 * h + e / 2] = from_float2<__half>(a, b);
+                            for (int e = 0; e < 16; e += 2) {
+                                const int at = 16 * (h & 1) + e;
+                                const float2 t = unpair(fma2(pair(__uint_as_float(s[h >> 1][at]), __uint_as_float(s[h >> 1][at + 1])), ff, aa));
+                                const float a = ex2(t.x), b = ex2(t.y);
+                                sum = add2(sum, pair(a, b));
+                                p[8 * h + e / 2] = from_float2<__half>(a, b);
+                            }
+                            const float2 both = unpair(sum);
+                            sums[h] = both.x + both.y;
                         }
-                        const float2 both = unpair(sum);
-                        l = fmaf(both.x + both.y, sc.z, l);
+                        if (look || !__any_sync(0xffffffffu, fmaxf(fmaxf(sums[0], sums[1]), fmaxf(sums[2], sums[3])) > kMostSum)) break;
+                        look = true;
                     }
+                    if (!ok) break;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) l = fmaf(sums[h], sh.scales[ring][4 * part + h].z, l);
                     tm_store32(s_at + 32u * part, p);        // over columns that have been read
                     tm_wait_store();
                     tc_fence_before();
@@ -588,8 +603,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             const int64_t out_row = unit.row0 + (int)(r / q.group);
             const uint32_t query_head = unit.head * q.group + r % q.group;
             constexpr uint32_t kPartial = kPromptRows * (kDim + 2u);
-            float* mine = partials + (uint64_t)(blockIdx.x * 2u + (unit.from == 0u ? 1u : 0u)) * kPartial + (half * 128u + row) * kDim;
-            float* mine_stat = mine - (half * 128u + row) * kDim + kPromptRows * kDim + (half * 128u + row) * 2u;
+            // a partial result: sums as [dim / 4][row] quadruples, so that a warp's rows lie side by side, then M and L of each row
+            const uint32_t at = half * 128u + row;
+            float* mine = partials + (uint64_t)(blockIdx.x * 2u + (unit.from == 0u ? 1u : 0u)) * kPartial;
             unsigned char* out = q.out + out_row * q.out_row + (int64_t)query_head * q.out_head;
             float* lse = q.lse && real ? q.lse + (uint64_t)out_row * q.heads + query_head : nullptr;
             const float by = l == 0.f ? 0.f : ref * __frcp_rn(l);
@@ -612,8 +628,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 } else if (real) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
-                        __stcg((float4*)(mine + 32u * c + e), make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]),
-                                                                          __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3])));
+                        __stcg((float4*)mine + (8u * c + e / 4) * kPromptRows + at,
+                               make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3])));
                 }
             }
             __syncwarp();
@@ -624,7 +640,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 if (lane == 0) bar_arrive(&sh.unit_free[un & 3u]);
                 continue;
             }
-            if (real) __stcg((float2*)mine_stat, make_float2(m, l));
+            if (real) __stcg((float2*)(mine + kPromptRows * kDim) + at, make_float2(m, l));
             const uint32_t c0 = shares.owner(unit.first), c1 = shares.owner(unit.end - 1u);
             __threadfence();
             ok = meet();
@@ -641,7 +657,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 __threadfence();
                 // block c0 left the unit's beginning in its second place, the others theirs in the first
                 auto place = [&](uint32_t c) { return partials + (uint64_t)(c * 2u + (c == c0 ? 1u : 0u)) * kPartial; };
-                const uint32_t at = half * 128u + row;
                 float top = -INFINITY, sum = 0.f;
                 for (uint32_t c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(place(c) + kPromptRows * kDim + at * 2u));
                 const float base = top == -INFINITY ? 0.f : top;
@@ -659,7 +674,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                         const float* p = place(c);
                         float4 a[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) a[e] = __ldcg((const float4*)(p + at * kDim + d) + e);
+                        for (int e = 0; e < 8; ++e) a[e] = __ldcg((const float4*)p + (d / 4 + e) * kPromptRows + at);
                         const float w = ex2(__ldcg(p + kPromptRows * kDim + at * 2u) - base);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
