@@ -14,6 +14,8 @@
 // whose values are 2^100 times smaller than another's would lose its weight in L.
 #pragma once
 
+#include <atomic>
+
 #include "entro_kv_common.cuh"
 
 namespace entro {
@@ -109,6 +111,19 @@ __device__ __forceinline__ Span span_of(int first, int last, uint32_t window, ui
 __device__ __forceinline__ bool sees(int position, int j, uint32_t window, uint32_t sinks)
 {
     return j <= position && (window == 0u || (int64_t)j > (int64_t)position - (int64_t)window || (uint32_t)j < sinks);
+}
+
+// Lets a kernel have that much dynamic shared memory on the current device; `allowed` remembers the devices.
+inline cudaError_t allow_shared(const void* kernel, uint32_t bytes, std::atomic<uint64_t>& allowed)
+{
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (device & 63);
+    if (allowed.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 // x pieces of work in equal shares for `parts` blocks: the first `more` get one more.

@@ -17,12 +17,13 @@ struct KvWorkHeader {
     uint32_t pairs;                 // page copies planned by fork / compact
     uint32_t pad[30];
     uint32_t part[128];             // per-CTA counts of the planning cluster
-    uint32_t arrived[1024];         // attention: partial results of a split unit that are in place (zero between calls)
+    // attention: partial results of a split unit that are in place (zero between calls)
+    uint32_t prompt_arrived[512], token_arrived[4][4096];
 };
 constexpr uint64_t kKvWorkRegion = (sizeof(KvWorkHeader) + 255) / 256 * 256;
 
-// Room for attention's partial results.  Single tokens: 512 blocks, two each, 16 rows of at most 128 + 2 floats;
-// prompts: 160 blocks, two each, 256 rows.
+// Room for attention's partial results.  Single tokens: at most 4096 shares, two each, of the call's rows (1 .. 16, and
+// half as many shares above 8) of at most 128 + 2 floats; prompts: 160 blocks, two each, 256 rows.
 constexpr uint64_t kKvPartialBytes = 160ull * 2 * 256 * 130 * 4;
 
 struct Kv {

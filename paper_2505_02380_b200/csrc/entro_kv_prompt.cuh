@@ -40,12 +40,10 @@ constexpr uint32_t kSlabBytes = 128 * 128;       // 128 rows of 64 fp16 numbers
 constexpr int kSoftmaxRegisters = 176, kConvertRegisters = 80, kProductRegisters = 80;
 static_assert(256 * kSoftmaxRegisters + 128 * kConvertRegisters + 128 * kProductRegisters <= 512 * 128, "no more than the launch has");
 constexpr uint32_t kWaitLimit = 1u << 20;        // tries of a barrier wait (each may suspend) before the kernel gives up
-// A row's maximum is moved only when it has to be: P (at most the sum of 16 columns) may reach 2^15 in fp16.  A move
-// waits for the product before and costs its half about 4000 cycles (at a growth of 2^8 every tenth piece had one), and
-// looking for the maximum at every piece costs a quarter of the softmax's instructions.  Once a sum has passed 2^15 the
-// maximum has grown by at least 2^11, so that the look that follows moves it.
-constexpr float kMostSum = 32768.f, kGrowth = 8.f;
-constexpr uint32_t kPromptArrived = 512;         // first counter of KvWorkHeader::arrived that is this kernel's
+// A row's maximum is moved only when it has to be, when a sum of 16 columns of P has passed 2^15 (fp16 ends at 2^16).
+// A move waits for the product before and costs its half about 4000 cycles (at a growth of 2^8 every tenth piece had
+// one), and looking for the maximum at every piece would cost a quarter of the softmax's instructions.
+constexpr float kMostSum = 32768.f;
 
 template <int kDim>
 constexpr uint32_t kPromptSlabs = kDim == 64 ? 1 : 2;
@@ -493,7 +491,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             __syncwarp();
             if (lane == 0) bar_arrive(&sh.q_empty[my_q % 3u]);
 
-            float m = -INFINITY, l = 0.f;
+            float m = real ? -INFINITY : 0.f, l = 0.f;
             for (uint32_t j = 0; j < pieces; ++j, ++piece_count, ++s_count) {
                 __syncwarp();
                 const uint32_t ring = piece_count & 3u;
@@ -516,7 +514,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                     // passes kMostSum (or nothing was seen before) the maximum is looked for, and P made again.
                     uint32_t p[32];
                     float sums[4];
-                    bool look = __any_sync(0xffffffffu, m == -INFINITY);
+                    bool look = false, mine = false;     // some row's of the warp, this row's
 #pragma unroll 1
                     for (;;) {
                         uint32_t s[2][32];
@@ -537,7 +535,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                                 for (int e = 1; e < 16; ++e) best = fmaxf(best, __uint_as_float(s[h >> 1][16 * (h & 1) + e]));
                                 top = fmaxf(top, fmaf(best, fmaxf(sc.x * row_factor, 1e-37f), sc.y));
                             }
-                            if (!(top > m + kGrowth || (m == -INFINITY && top > -INFINITY))) top = m;
+                            if (!(mine && top > m)) top = m;
                             if (__any_sync(0xffffffffu, top != m)) {
                                 const float shrink = top == m ? 1.f : ex2(m - top);
                                 l *= shrink;
@@ -578,8 +576,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                             const float2 both = unpair(sum);
                             sums[h] = both.x + both.y;
                         }
-                        if (look || !__any_sync(0xffffffffu, fmaxf(fmaxf(sums[0], sums[1]), fmaxf(sums[2], sums[3])) > kMostSum)) break;
-                        look = true;
+                        if (look) break;
+                        // each row by itself: what happens in one does not change another's rounding
+                        mine = m == -INFINITY || fmaxf(fmaxf(sums[0], sums[1]), fmaxf(sums[2], sums[3])) > kMostSum;
+                        look = __any_sync(0xffffffffu, mine);
+                        if (!look) break;
                     }
                     if (!ok) break;
 #pragma unroll
@@ -646,7 +647,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             ok = meet();
             if (!ok) break;
             if (row == 0) {
-                uint32_t* counter = &kv.head->arrived[kPromptArrived + 2u * c0 + half];
+                uint32_t* counter = &kv.head->prompt_arrived[2u * c0 + half];
                 const uint32_t was = atomicAdd(counter, 1u);
                 sh.last[half] = was == c1 - c0;
                 if (was == c1 - c0) *counter = 0u;
@@ -1006,8 +1007,8 @@ cudaError_t launch_prompt(const Kv& kv, const KvBatch& batch, const Query& q, ui
                           cudaStream_t s)
 {
     auto* kernel = prompt_attention_kernel<T, kDim>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPromptSmem<kDim>);
-    if (e != cudaSuccess) return e;
+    static std::atomic<uint64_t> allowed;
+    if (cudaError_t e = allow_shared((const void*)kernel, kPromptSmem<kDim>, allowed)) return e;
     kernel<<<min(kPromptBlocks, sm_count), kPromptThreads, kPromptSmem<kDim>, s>>>(kv, batch, q, partials, few_rows);
     return cudaGetLastError();
 }

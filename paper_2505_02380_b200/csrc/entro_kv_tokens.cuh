@@ -1,20 +1,22 @@
 // Attention of few rows per sequence (a token step): the cache is read once, at memory speed.
 //
-// A unit is a sequence and a key/value head: its rows (new tokens times query heads of the group,
-// at most 8 * kTiles) against all tokens they see, in slices of 16 tokens.  All slices of all units
-// form one line that is cut into equal shares, one per block, whatever the lengths; a unit that is
-// cut leaves partial results (M, L, sums) that the block arriving last joins, in the order of the
-// shares, so results do not depend on who came first.
+// A unit is a sequence and a key/value head: its rows (new tokens times query heads of the group)
+// against all tokens they see, in slices of 16 tokens.  All slices of all units form one line that is
+// cut into equal shares, one per WARP, whatever the lengths; a unit that is cut leaves partial results
+// (M, L, sums), which are joined eight at a time: of eight neighbours the warp that arrives last joins
+// them in order, and so on up.  So results do not depend on who came first, and warps never wait for one
+// another.  (With units joined by whole blocks, starting and ending one cost every warp of the block about
+// 6 us of barriers and fences, and blocks with many short sequences were last by far; joined by one warp,
+// 26 to 38 partial results took 14 to 20 us behind everything else; joined by a second kernel, 5 to 7 us.)
 //
-// Inside a block every warp takes slices of its own (8 warps, every eighth slice) with statistics of
-// its own, joined at the unit's end.  Products run on m16n8k16 with the tokens as rows, so that eight
-// query heads fill a tile:  S^T[16 tokens, 8] = K' Q^T and O^T[dim, 8] += V'^T P^T.  The matrix unit is
-// far from busy: the bound is memory, then the byte-to-fp16 conversion (1 to 1.25 instructions per
-// code).  Any permutation of the inner index is allowed if both operands share it, so a thread's 16
-// consecutive bytes of a key row serve four products, and a thread's 16 bytes of four value rows eight.
+// Products run on m16n8k16 with the tokens as rows, so that eight query heads fill a tile:
+// S^T[16 tokens, 8] = K' Q^T and O^T[dim, 8] += V'^T P^T.  The matrix unit is far from busy: the bound is
+// memory, then the byte-to-fp16 conversion (1 to 1.25 instructions per code).  Any permutation of the
+// inner index is allowed if both operands share it, so a thread's 16 consecutive bytes of a key row serve
+// four products, and a thread's 16 bytes of four value rows eight.
 // Each warp keeps a ring of slices of its own in shared memory, filled by asynchronous 16-byte copies
-// two slices ahead; rows are 16 bytes longer there than in the cache, which spreads the four value rows
-// of a load over the banks.  No barrier until the unit's end.
+// slices ahead; rows are 16 bytes longer there than in the cache, which spreads the four value rows of a
+// load over the banks.
 #pragma once
 
 #include "entro_kv_attention.cuh"
@@ -24,13 +26,16 @@ namespace {
 
 constexpr uint32_t kTokenWarps = 8, kTokenThreads = 32 * kTokenWarps;
 constexpr uint32_t kTokenRows = 16;             // most rows of a unit
-constexpr uint32_t kTokenBlocks = 512;          // most blocks of a launch
-constexpr uint32_t kTokenMinSlices = 16;        // a share is not made smaller than this
-// Starting and ending a unit costs a block about as much time as this many slices; on the line a unit
-// is that much longer than its slices, or a block with many short sequences would be last by far.
-constexpr uint32_t kTokenUnitCost = 12;
+constexpr uint32_t kTokenShares = 4096;         // most shares (warps) of a launch
+constexpr uint32_t kTokenMinShare = 8;          // a share is not made smaller than this (in slices)
+// Starting and ending a unit costs a warp about as much time as this many slices; on the line a unit is that much
+// longer than its slices.
+constexpr uint32_t kTokenUnitCost = 4;
+constexpr uint32_t kJoin = 8;                   // partial results joined at a time
+constexpr uint32_t kTokenPrefix = 512;          // entries of the table of line places
 
-static_assert(kKvPartialBytes >= 4ull * kTokenBlocks * 2 * kTokenRows * 130, "a block leaves at most two partial results");
+static_assert(kTokenShares <= kJoin * kJoin * kJoin * kJoin && kTokenShares == sizeof(KvWorkHeader{}.token_arrived[0]) / 4u, "four levels of joining");
+static_assert(kKvPartialBytes >= 4ull * kTokenShares * 2 * (kTokenRows * 130 + 4) / 2, "a warp leaves at most two partial results");
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
@@ -128,7 +133,7 @@ __device__ __forceinline__ void load_value_row(uint32_t row, uint32_t g, uint32_
 }
 
 // A ring stage: 16 key rows, 16 value rows, the two scales.  Two blocks of 8 warps (one tile) or one (two tiles) share
-// the SM's 227 KB.
+// the SM's 227 KB with the table of line places.
 template <int kDim>
 constexpr uint32_t kTokenRowBytes = kDim + 16;
 template <int kDim>
@@ -156,46 +161,48 @@ __device__ __forceinline__ TokenSeq token_seq(const Kv& kv, const KvBatch& batch
     return s;
 }
 
+// Dims d .. d + 3 of row r of a unit: the sums v, relative to maximum `top` and with the softmax sum `sum`.
+template <typename T>
+__device__ __forceinline__ void finish_row(const Query& q, int row0, uint32_t head, float ref, uint32_t r, uint32_t d, float4 v, float top, float sum)
+{
+    const float by = sum == 0.f ? 0.f : ref * __frcp_rn(sum);
+    const uint32_t token = r / q.group, query_head = head * q.group + r - token * q.group;
+    const int64_t row = row0 + (int)token;
+    *(uint2*)(q.out + row * q.out_row + (int64_t)query_head * q.out_head + 2u * d) =
+        make_uint2(from_float2<T>(v.x * by, v.y * by), from_float2<T>(v.z * by, v.w * by));
+    if (d == 0 && q.lse) q.lse[(uint64_t)row * q.heads + query_head] = sum == 0.f ? -INFINITY : kLn2 * (top + log2f(sum));
+}
+
+// Floats of one partial result: sums [rows][dim], then (M, L) [rows]; a multiple of 16 bytes.
+__host__ __device__ constexpr uint32_t token_place(uint32_t rows, uint32_t dim) { return (rows * (dim + 2u) + 3u) / 4u * 4u; }
+
 template <typename T, int kDim, int kTiles>
 __global__ void __launch_bounds__(kTokenThreads, kTiles == 1 ? 2 : 1)
-    token_attention_kernel(Kv kv, KvBatch batch, Query q, float* partials)
+    token_attention_kernel(Kv kv, KvBatch batch, Query q, float* partials, uint32_t most_rows)
 {
     constexpr uint32_t kCols = 8 * kTiles;
     constexpr int kSteps = kDim / 16;            // products of a slice's first matrix product; words of a key row
     constexpr int kWords = kDim / 32;            // words of a value row
-    constexpr uint32_t kStride = kDim + 4;
     constexpr int kStages = kTokenStages<kDim, kTiles>;
     constexpr uint32_t kRow = kTokenRowBytes<kDim>, kStage = kTokenStageBytes<kDim>;
-    extern __shared__ __align__(16) float joined[];              // [warps][cols][stride], where the rings lie until then
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(joined) + (threadIdx.x >> 5) * kStages * kStage;
-    __shared__ float stat_m[kTokenWarps][kCols], stat_l[kTokenWarps][kCols];
-    __shared__ uint32_t found_b, found_before, is_last, warp_sums[kTokenWarps];
+    extern __shared__ __align__(16) unsigned char rings[];
+    __shared__ uint32_t prefix[kTokenPrefix + 1u], warp_sums[kTokenWarps];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3u;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(rings) + warp * kStages * kStage;
 
-    // ---- this block's share of the line of slices
-    auto slices_of = [&](uint32_t b) {
+    // ---- the line: prefix[i] = what the sequences before i * per take of it
+    auto line_length = [&](uint32_t b) {
         Span span;
         const uint32_t n = token_seq(kv, batch, q, b, kCols, &span).slices;
         return n ? (n + kTokenUnitCost) * kv.heads : 0u;
     };
-    uint32_t mine = 0;
-    for (uint32_t b = threadIdx.x; b < batch.n; b += kTokenThreads) mine += slices_of(b);
-#pragma unroll
-    for (int s = 16; s; s >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, s);
-    if (lane == 0) warp_sums[warp] = mine;
-    __syncthreads();
+    const uint32_t per = (batch.n + kTokenPrefix - 1u) / kTokenPrefix, entries = (batch.n + per - 1u) / per;
     uint32_t all = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < kTokenWarps; ++w) all += warp_sums[w];
-    const uint32_t parts = min(gridDim.x, (all + kTokenMinSlices - 1u) / kTokenMinSlices);
-    if (blockIdx.x >= parts) return;
-    const Shares shares(all, parts);
-    uint32_t x = shares.start(blockIdx.x);
-    const uint32_t x_end = shares.start(blockIdx.x + 1u);
-    // sequence that slice x belongs to
-    for (uint32_t base = 0, before = 0; base < batch.n; base += kTokenThreads) {
-        const uint32_t b = base + threadIdx.x;
-        const uint32_t w = b < batch.n ? slices_of(b) : 0u;
+    for (uint32_t base = 0; base < entries; base += kTokenThreads) {
+        const uint32_t entry = base + threadIdx.x;
+        uint32_t w = 0;
+        if (entry < entries)
+            for (uint32_t b = entry * per; b < min(batch.n, (entry + 1u) * per); ++b) w += line_length(b);
         uint32_t sum = w;
 #pragma unroll
         for (int s = 1; s < 32; s <<= 1) {
@@ -211,16 +218,29 @@ __global__ void __launch_bounds__(kTokenThreads, kTiles == 1 ? 2 : 1)
             if (i < warp) sum += warp_sums[i];
             chunk += warp_sums[i];
         }
-        const uint32_t from = before + sum - w;
-        if (x >= from && x < from + w) {
-            found_b = b;
-            found_before = from;
-        }
-        before += chunk;
-        if (x < before) break;       // the same for all threads
+        if (entry < entries) prefix[entry + 1u] = all + sum;
+        all += chunk;
     }
+    if (threadIdx.x == 0) prefix[0] = 0u;
     __syncthreads();
-    uint32_t b = found_b, seq_start = found_before;
+
+    // ---- this warp's share.  Neighbouring shares go to different blocks, so that few shares spread over all SMs
+    const uint32_t parts = min(min(gridDim.x * kTokenWarps, kTokenShares), (all + kTokenMinShare - 1u) / kTokenMinShare);
+    const uint32_t mine = warp * gridDim.x + blockIdx.x;
+    if (mine >= parts) return;
+    const Shares shares(all, parts);
+    uint32_t x = shares.start(mine);
+    const uint32_t x_end = shares.start(mine + 1u);
+    // the last entry that begins at or before x (entries without length share their place with the next: the last is the one)
+    uint32_t at = 0;
+    for (uint32_t left = entries; left > 1u;) {
+        const uint32_t stride = (left + 31u) / 32u, probe = at + lane * stride;
+        const uint32_t in = __ballot_sync(0xffffffffu, lane * stride < left && prefix[probe] <= x);
+        const uint32_t k = 31u - __clz(in);
+        at += k * stride;
+        left = min(stride, left - k * stride);
+    }
+    uint32_t b = at * per, seq_start = prefix[at];
 
     Span span;
     TokenSeq seq = token_seq(kv, batch, q, b, kCols, &span);
@@ -241,6 +261,61 @@ __global__ void __launch_bounds__(kTokenThreads, kTiles == 1 ? 2 : 1)
         }
         const uint32_t rows = (uint32_t)seq.rows * q.group;
         const int first = seq.len - seq.rows;                    // position of the first row
+
+        float o[kSteps][kTiles][4];
+        float m[kTiles][2], l[kTiles][2];
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
+            m[n][0] = m[n][1] = -INFINITY;
+            l[n][0] = l[n][1] = 0.f;
+        }
+
+        // ---- slices i_begin .. i_end - 1 of the unit
+        const int last = seq.len - 1;
+        const uint32_t i_begin = x - unit_start, i_end = seq.len > 0 ? stop - unit_start : 0u;
+        // slices that all rows see whole: number whole_from and whole_count - 1 more
+        uint32_t whole_from = 0, whole_to = first >= 0 ? ((uint32_t)first + 1u) >> 4 : 0u;
+        if (q.window) {
+            const int64_t outside = (int64_t)last - (int64_t)q.window;           // up to here the last row does not see
+            whole_from = outside < 0 ? 0u : (uint32_t)((outside + 16) >> 4);
+        }
+        whole_from = max(whole_from, span.low) - span.low + span.sinks;
+        whole_to = max(whole_to, span.low) - span.low + span.sinks;
+        const uint32_t whole_count = whole_to > whole_from ? whole_to - whole_from : 0u;
+        const int32_t* table_row = kv.table + (uint64_t)max(seq.slot, 0) * kv.width;
+        const uint64_t page_bytes = kv.page_bytes(), to_values = (uint64_t)kv.heads * kv.head_bytes();
+        const uint8_t* lane_codes = kv.codes + head * kv.head_bytes() + lane * 16u;
+        const float* lane_scales = kv.scales + head + (lane & 1u) * kv.heads;
+        const uint32_t in_page = kv.page() / 16u - 1u, to_block = kv.page_shift - 4u;
+        auto page_at = [&](uint32_t idx) -> int {
+            if (idx >= i_end) return -1;
+            const uint32_t block = span.piece(idx) >> to_block;
+            if (block >= kv.width) return -1;
+            const int p = __ldg(table_row + block);
+            return (uint32_t)p < kv.pages ? p : -1;
+        };
+        // slice idx, whose page is `page`, into a stage; one commit group per call
+        auto fetch = [&](int page, uint32_t idx, uint32_t stage) {
+            if (page >= 0) {
+                const uint8_t* k = lane_codes + (uint64_t)(uint32_t)page * page_bytes + (span.piece(idx) & in_page) * (16u * kDim);
+#pragma unroll
+                for (int c = 0; c < kDim / 32; ++c) {
+                    const uint32_t chunk = lane + 32u * c, at = chunk / (kDim / 16u) * kRow + chunk % (kDim / 16u) * 16u;
+                    copy16(stage + at, k + 512u * c);
+                    copy16(stage + 16u * kRow + at, k + to_values + 512u * c);
+                }
+                if (lane < 2u) copy4(stage + 32u * kRow + lane * 4u, lane_scales + (uint64_t)(uint32_t)page * 2u * kv.heads);
+            }
+            copies_commit();
+        };
+        const float ref = value_reference(kv, seq.slot, span.piece(0) >> to_block, head), by_ref = __frcp_rn(ref);
+        int pages[kStages];          // of the slices in the ring and, last, of the next one to fetch
+#pragma unroll
+        for (int c = 0; c < kStages; ++c) pages[c] = page_at(i_begin + c);
+#pragma unroll
+        for (int c = 0; c < kStages - 1; ++c) fetch(pages[c], i_begin + c, ring + c * kStage);
 
         // ---- the rows as the second operand; columns 2t, 2t + 1 of each tile are this lane's
         uint32_t qf[kTiles][kSteps][2];
@@ -291,62 +366,16 @@ __global__ void __launch_bounds__(kTokenThreads, kTiles == 1 ? 2 : 1)
             }
         }
 
-        float o[kSteps][kTiles][4];
-        float m[kTiles][2], l[kTiles][2];
-#pragma unroll
-        for (int n = 0; n < kTiles; ++n) {
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
-            m[n][0] = m[n][1] = -INFINITY;
-            l[n][0] = l[n][1] = 0.f;
-        }
-
-        // ---- slices x + warp, x + warp + 8, ...
-        const int last = seq.len - 1;
-        const int64_t open_from = q.window ? (int64_t)last - (int64_t)q.window : -1;   // later positions are in every row's window
-        uint32_t i = x + warp - unit_start;
-        const uint32_t i_end = seq.len > 0 ? stop - unit_start : 0u;
-        const int32_t* table_row = kv.table + (uint64_t)max(seq.slot, 0) * kv.width;
-        const uint64_t page_bytes = kv.page_bytes(), to_values = (uint64_t)kv.heads * kv.head_bytes();
-        const uint8_t* lane_codes = kv.codes + head * kv.head_bytes() + lane * 16u;
-        const float* lane_scales = kv.scales + head + (lane & 1u) * kv.heads;
-        const uint32_t in_page = kv.page() / 16u - 1u, to_block = kv.page_shift - 4u;
-        auto page_at = [&](uint32_t idx) -> int {
-            if (idx >= i_end) return -1;
-            const uint32_t block = span.piece(idx) >> to_block;
-            if (block >= kv.width) return -1;
-            const int p = __ldg(table_row + block);
-            return (uint32_t)p < kv.pages ? p : -1;
-        };
-        // slice idx, whose page is `page`, into a stage; one commit group per call
-        auto fetch = [&](int page, uint32_t idx, uint32_t stage) {
-            if (page >= 0) {
-                const uint8_t* k = lane_codes + (uint64_t)(uint32_t)page * page_bytes + (span.piece(idx) & in_page) * (16u * kDim);
-#pragma unroll
-                for (int c = 0; c < kDim / 32; ++c) {
-                    const uint32_t chunk = lane + 32u * c, at = chunk / (kDim / 16u) * kRow + chunk % (kDim / 16u) * 16u;
-                    copy16(stage + at, k + 512u * c);
-                    copy16(stage + 16u * kRow + at, k + to_values + 512u * c);
-                }
-                if (lane < 2u) copy4(stage + 32u * kRow + lane * 4u, lane_scales + (uint64_t)(uint32_t)page * 2u * kv.heads);
-            }
-            copies_commit();
-        };
-        const float ref = value_reference(kv, seq.slot, span.piece(0) >> to_block, head), by_ref = __frcp_rn(ref);
-        int pages[kStages];          // of the slices in the ring and, last, of the next one to fetch
-#pragma unroll
-        for (int c = 0; c < kStages; ++c) pages[c] = page_at(i + c * kTokenWarps);
-#pragma unroll
-        for (int c = 0; c < kStages - 1; ++c) fetch(pages[c], i + c * kTokenWarps, ring + c * kStage);
+        bool unseen = true;          // some column has seen nothing yet
         uint32_t stage = ring, stage_in = ring + (kStages - 1) * kStage;
-        for (; i < i_end; i += kTokenWarps) {
+        for (uint32_t i = i_begin; i < i_end; ++i) {
             copies_wait<kStages - 2>();
             __syncwarp();            // every lane's copies of this slice are in place, and the stage before it has been read
             const int page = pages[0];
-            fetch(pages[kStages - 1], i + (kStages - 1) * kTokenWarps, stage_in);
+            fetch(pages[kStages - 1], i + kStages - 1, stage_in);
 #pragma unroll
             for (int c = 0; c + 1 < kStages; ++c) pages[c] = pages[c + 1];
-            pages[kStages - 1] = page_at(i + kStages * kTokenWarps);
+            pages[kStages - 1] = page_at(i + kStages);
 
             float s[kTiles][4];
 #pragma unroll
@@ -362,54 +391,70 @@ __global__ void __launch_bounds__(kTokenThreads, kTiles == 1 ? 2 : 1)
                     for (int n = 0; n < kTiles; ++n) mma_16816(s[n], a, qf[n][j][0], qf[n][j][1]);
                 }
             }
-            const int j0 = (int)(span.piece(i) * 16u);
             const bool there = page >= 0;
-            const bool whole = there && j0 + 15 <= first && (j0 > open_from || (uint32_t)j0 + 15u < q.sinks);
             const float key_scale = __uint_as_float(lds4(stage + 32u * kRow));
             const float rel = there ? relative_scale(__uint_as_float(lds4(stage + 32u * kRow + 4u)), by_ref) : 1.f;
             const float lv = lg2(rel), inv = rcp(rel);
-
-            uint32_t pb[kTiles][2];
-            float shrink[kTiles][2];
-            bool moved = false;
+            float u[kTiles][4], p[kTiles][4];
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) {
-                float u[4];
+            for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) u[c] = fmaf(s[n][c], key_scale * factor[n][c & 1], lv);
-                if (!whole) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        if (!there || !sees(position[n][c & 1], j0 + (int)g + 8 * (c >> 1), q.window, q.sinks)) u[c] = -INFINITY;
-                }
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float top = fmaxf(u[c], u[c + 2]);
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                    const float up = fmaxf(m[n][c], top);
-                    const float base = up == -INFINITY ? 0.f : up;
-                    moved |= up != m[n][c];
-                    shrink[n][c] = ex2(m[n][c] - base);
-                    m[n][c] = up;
-                    u[c] = ex2(u[c] - base);
-                    u[c + 2] = ex2(u[c + 2] - base);
-                    l[n][c] = fmaf(u[c] + u[c + 2], inv, l[n][c] * shrink[n][c]);
-                }
-                pb[n][0] = transpose_8x8(from_float2<__half>(u[0], u[1]));
-                pb[n][1] = transpose_8x8(from_float2<__half>(u[2], u[3]));
-            }
-            if (__any_sync(0xffffffffu, moved)) {
+                for (int c = 0; c < 4; ++c) u[n][c] = fmaf(s[n][c], key_scale * factor[n][c & 1], lv);
+            if (!there || i - whole_from >= whole_count) {
+                const int j0 = (int)(span.piece(i) * 16u);
 #pragma unroll
                 for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-                    for (int j = 0; j < kSteps; ++j) {
-                        o[j][n][0] *= shrink[n][0];
-                        o[j][n][1] *= shrink[n][1];
-                        o[j][n][2] *= shrink[n][0];
-                        o[j][n][3] *= shrink[n][1];
+                    for (int c = 0; c < 4; ++c)
+                        if (!there || !sees(position[n][c & 1], j0 + (int)g + 8 * (c >> 1), q.window, q.sinks)) u[n][c] = -INFINITY;
+            }
+            // P relative to the maximum as it is known; only when one leaves fp16's range (or a column has seen nothing
+            // yet) the maximum is looked for, which takes three exchanges between lanes for each column
+            bool look = unseen;
+            if (!look) {
+                float most = 0.f;
+#pragma unroll
+                for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        p[n][c] = ex2(u[n][c] - m[n][c & 1]);
+                        most = fmaxf(most, p[n][c]);
                     }
+                look = __any_sync(0xffffffffu, most > 32768.f);
+            }
+            if (look) {
+                bool none = false;
+#pragma unroll
+                for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float top = fmaxf(u[n][c], u[n][c + 2]);
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                        // each column by itself: what happens in one does not change another's rounding
+                        if (!(top > m[n][c] + 15.f || m[n][c] == -INFINITY)) top = m[n][c];
+                        const float base = top == -INFINITY ? 0.f : top, shrink = ex2(m[n][c] - base);
+                        none |= top == -INFINITY;
+                        m[n][c] = top;
+                        p[n][c] = ex2(u[n][c] - base);
+                        p[n][c + 2] = ex2(u[n][c + 2] - base);
+                        l[n][c] *= shrink;
+#pragma unroll
+                        for (int j = 0; j < kSteps; ++j) {
+                            o[j][n][c] *= shrink;
+                            o[j][n][c + 2] *= shrink;
+                        }
+                    }
+                unseen = __any_sync(0xffffffffu, none);
+            }
+            uint32_t pb[kTiles][2];
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) {
+                l[n][0] = fmaf(p[n][0] + p[n][2], inv, l[n][0]);
+                l[n][1] = fmaf(p[n][1] + p[n][3], inv, l[n][1]);
+                pb[n][0] = transpose_8x8(from_float2<__half>(p[n][0], p[n][1]));
+                pb[n][1] = transpose_8x8(from_float2<__half>(p[n][2], p[n][3]));
             }
             uint32_t vw[4][kWords];
             load_value_row<kDim>(stage + (16u + 2u * t) * kRow, g, vw[0]);
@@ -433,119 +478,123 @@ __global__ void __launch_bounds__(kTokenThreads, kTiles == 1 ? 2 : 1)
             stage = stage + kStage == ring + kStages * kStage ? ring : stage + kStage;
         }
 
-        // ---- the warps' results become the block's
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                float sum = l[n][c];
-                sum += __shfl_xor_sync(0xffffffffu, sum, 4);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 8);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 16);
-                if (g == 0) {
-                    stat_m[warp][8 * n + 2 * t + c] = m[n][c];
-                    stat_l[warp][8 * n + 2 * t + c] = sum;
-                }
+                l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], 4);
+                l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], 8);
+                l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], 16);
             }
-        __syncthreads();
-#pragma unroll
-        for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const uint32_t col = 8u * n + 2u * t + c;
-                float top = -INFINITY;
-#pragma unroll
-                for (uint32_t w = 0; w < kTokenWarps; ++w) top = fmaxf(top, stat_m[w][col]);
-                const float f = top == -INFINITY ? 0.f : ex2(m[n][c] - top);
-                float* to = joined + (warp * kCols + col) * kStride;
-#pragma unroll
-                for (int w = 0; w < kWords; ++w)
-                    *(float4*)(to + value_dim<kDim>(w, g)) =
-                        make_float4(o[2 * w][n][c] * f, o[2 * w][n][c + 2] * f, o[2 * w + 1][n][c] * f, o[2 * w + 1][n][c + 2] * f);
-            }
-        __syncthreads();
-        const bool complete = x == unit_start && stop == unit_end;
-        // of a block's two places the first is for a unit that began in another block, the second for one that goes on in the next
-        const uint32_t row_floats = kCols * (kDim + 2u);
-        float* partial = partials + (uint64_t)(blockIdx.x * 2u + (x == unit_start ? 1u : 0u)) * row_floats;
-        auto finish = [&](uint32_t r, uint32_t d, float4 v, float top, float sum) {
-            const float by = sum == 0.f ? 0.f : ref * __frcp_rn(sum);
-            const int64_t row = seq.row0 + (int)(r / q.group);
-            const uint32_t query_head = head * q.group + r % q.group;
-            uint2 two = make_uint2(from_float2<T>(v.x * by, v.y * by), from_float2<T>(v.z * by, v.w * by));
-            *(uint2*)(q.out + row * q.out_row + (int64_t)query_head * q.out_head + 2u * d) = two;
-            if (d == 0 && q.lse) q.lse[(uint64_t)row * q.heads + query_head] = sum == 0.f ? -INFINITY : kLn2 * (top + log2f(sum));
+        __syncwarp();                // the ring has been read
+        // a lane's four dims of word w and column (n, c)
+        auto quad = [&](int w, int n, int c) {
+            return make_float4(o[2 * w][n][c], o[2 * w][n][c + 2], o[2 * w + 1][n][c], o[2 * w + 1][n][c + 2]);
         };
-        for (uint32_t e = threadIdx.x; e < rows * (kDim / 4u); e += kTokenThreads) {
-            const uint32_t r = e / (kDim / 4u), d = 4u * (e - r * (kDim / 4u));
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            float top = -INFINITY, sum = 0.f;
+        if (x == unit_start && stop == unit_end) {
 #pragma unroll
-            for (uint32_t w = 0; w < kTokenWarps; ++w) top = fmaxf(top, stat_m[w][r]);
+            for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-            for (uint32_t w = 0; w < kTokenWarps; ++w) {
-                sum += stat_l[w][r] * (top == -INFINITY ? 0.f : ex2(stat_m[w][r] - top));
-                const float4 a = *(const float4*)(joined + (w * kCols + r) * kStride + d);
-                v.x += a.x;
-                v.y += a.y;
-                v.z += a.z;
-                v.w += a.w;
-            }
-            if (complete) {
-                finish(r, d, v, top, sum);
-            } else {
-                __stcg((float4*)(partial + r * kDim + d), v);
-                if (d == 0) {
-                    __stcg(partial + kCols * kDim + r, top);
-                    __stcg(partial + kCols * kDim + kCols + r, sum);
-                }
-            }
-        }
-        if (!complete) {
-            // the unit's shares: blocks c0 .. c1; the last one to arrive joins them in that order
-            const uint32_t c0 = shares.owner(unit_start), c1 = shares.owner(unit_end - 1u);
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                const uint32_t before = atomicAdd(&kv.head->arrived[c0], 1u);
-                is_last = before == c1 - c0;
-                if (is_last) kv.head->arrived[c0] = 0u;
-            }
-            __syncthreads();
-            if (is_last) {
-                __threadfence();
-                const float* from0 = partials + (uint64_t)(c0 * 2u + 1u) * row_floats;
-                const float* from1 = partials + (uint64_t)((c0 + 1u) * 2u) * row_floats;
-                const uint32_t others = c1 - c0;
-                for (uint32_t e = threadIdx.x; e < rows * (kDim / 4u); e += kTokenThreads) {
-                    const uint32_t r = e / (kDim / 4u), d = 4u * (e - r * (kDim / 4u));
-                    const float m0 = __ldcg(from0 + kCols * kDim + r);
-                    float top = m0;
-#pragma unroll 8
-                    for (uint32_t c = 0; c < others; ++c)
-                        top = fmaxf(top, __ldcg(from1 + (uint64_t)c * 2u * row_floats + kCols * kDim + r));
-                    const float base = top == -INFINITY ? 0.f : top;
-                    float f = ex2(m0 - base);
-                    float sum = __ldcg(from0 + kCols * kDim + kCols + r) * f;
-                    float4 v = __ldcg((const float4*)(from0 + r * kDim + d));
-                    v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-#pragma unroll 8
-                    for (uint32_t c = 0; c < others; ++c) {
-                        const float* p = from1 + (uint64_t)c * 2u * row_floats;
-                        const float mc = __ldcg(p + kCols * kDim + r), lc = __ldcg(p + kCols * kDim + kCols + r);
-                        const float4 a = __ldcg((const float4*)(p + r * kDim + d));
-                        f = ex2(mc - base);
-                        sum = fmaf(lc, f, sum);
-                        v.x = fmaf(a.x, f, v.x);
-                        v.y = fmaf(a.y, f, v.y);
-                        v.z = fmaf(a.z, f, v.z);
-                        v.w = fmaf(a.w, f, v.w);
+                for (int c = 0; c < 2; ++c)
+                    if (8u * n + 2u * t + c < rows) {
+#pragma unroll
+                        for (int w = 0; w < kWords; ++w)
+                            finish_row<T>(q, seq.row0, head, ref, 8u * n + 2u * t + c, value_dim<kDim>(w, g), quad(w, n, c), m[n][c], l[n][c]);
                     }
-                    finish(r, d, v, top, sum);
+            x = stop;
+            continue;
+        }
+        // A cut unit.  Of a warp's two places the first is for a unit that began in another share, the second for one
+        // that goes on in the next.
+        const uint32_t place = token_place(most_rows, kDim);
+        float* partial = partials + (uint64_t)(mine * 2u + (x == unit_start ? 1u : 0u)) * place;
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const uint32_t r = 8u * n + 2u * t + c;
+                if (r >= rows) continue;
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) __stcg((float4*)(partial + r * kDim + value_dim<kDim>(w, g)), quad(w, n, c));
+                if (g == 0) __stcg((float2*)(partial + most_rows * kDim) + r, make_float2(m[n][c], l[n][c]));
+            }
+        // the unit's shares are c0 .. c0 + many - 1; up the tree until this warp is not the last of its eight
+        const uint32_t c0 = shares.owner(unit_start), many = shares.owner(unit_end - 1u) - c0 + 1u;
+        uint32_t k = mine - c0, span8 = 1;       // this warp's result stands for shares c0 + k .. c0 + k + span8 - 1
+#pragma unroll 1
+        for (uint32_t level = 0;; ++level, span8 *= kJoin) {
+            const uint32_t first_of = k / (kJoin * span8) * (kJoin * span8);
+            const uint32_t count = min(kJoin, (many - first_of + span8 - 1u) / span8);
+            const bool top_level = count * span8 >= many;            // then first_of is 0
+            if (count > 1u) {
+                __threadfence();
+                __syncwarp();
+                uint32_t before = 0;
+                uint32_t* arrived = &kv.head->token_arrived[level][c0 + first_of];
+                if (lane == 0) before = atomicAdd(arrived, 1u);
+                if (__shfl_sync(0xffffffffu, before, 0) != count - 1u) break;
+                if (lane == 0) *arrived = 0u;
+                __threadfence();
+                // share c0's result lies in its second place, those of the others in their first
+                auto result = [&](uint32_t i) {
+                    const uint32_t c = first_of + i * span8;
+                    return partials + (uint64_t)((c0 + c) * 2u + (c == 0u ? 1u : 0u)) * place;
+                };
+                const uint32_t items = rows * (kDim / 4u);
+                for (uint32_t e0 = 0; e0 < items; e0 += 64u) {       // two items (four dims of a row) a lane, all results on their way at once
+                    float2 ml[2][kJoin];
+                    float4 a[2][kJoin];
+#pragma unroll
+                    for (uint32_t h = 0; h < 2u; ++h)
+#pragma unroll
+                        for (uint32_t i = 0; i < kJoin; ++i) {
+                            const uint32_t e = min(e0 + 32u * h + lane, items - 1u), r = e / (kDim / 4u), d = 4u * (e - r * (kDim / 4u));
+                            const float* p = result(min(i, count - 1u));
+                            ml[h][i] = __ldcg((const float2*)(p + most_rows * kDim) + r);
+                            a[h][i] = __ldcg((const float4*)(p + r * kDim + d));
+                        }
+#pragma unroll
+                    for (uint32_t h = 0; h < 2u; ++h) {
+                        const uint32_t e = e0 + 32u * h + lane, r = e / (kDim / 4u), d = 4u * (e - r * (kDim / 4u));
+                        float up = -INFINITY, sum = 0.f;
+                        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (uint32_t i = 0; i < kJoin; ++i) {
+                            if (i >= count) ml[h][i] = make_float2(-INFINITY, 0.f);
+                            up = fmaxf(up, ml[h][i].x);
+                        }
+                        const float low = up == -INFINITY ? 0.f : up;
+#pragma unroll
+                        for (uint32_t i = 0; i < kJoin; ++i) {
+                            const float f = ex2(ml[h][i].x - low);
+                            sum = fmaf(ml[h][i].y, f, sum);
+                            v.x = fmaf(a[h][i].x, f, v.x);
+                            v.y = fmaf(a[h][i].y, f, v.y);
+                            v.z = fmaf(a[h][i].z, f, v.z);
+                            v.w = fmaf(a[h][i].w, f, v.w);
+                        }
+                        if (e >= items) continue;
+                        if (top_level) {
+                            finish_row<T>(q, seq.row0, head, ref, r, d, v, up, sum);
+                        } else {             // into the ring for now: other lanes still read the place it goes to
+                            float* to = (float*)(rings + warp * kStages * kStage);
+                            *(float4*)(to + r * kDim + d) = v;
+                            if (d == 0u) *(float2*)(to + most_rows * kDim + 2u * r) = make_float2(up, sum);
+                        }
+                    }
+                }
+                if (!top_level) {
+                    __syncwarp();
+                    float* to = partials + (uint64_t)((c0 + first_of) * 2u + (first_of == 0u ? 1u : 0u)) * place;
+                    for (uint32_t e = lane; e < place / 4u; e += 32u)
+                        __stcg((float4*)to + e, *((const float4*)(rings + warp * kStages * kStage) + e));
+                    __syncwarp();
                 }
             }
+            if (top_level) break;
+            k = first_of;
         }
-        __syncthreads();             // shared memory is free for the next unit
+        __syncwarp();
         x = stop;
     }
 }
@@ -558,15 +607,9 @@ cudaError_t launch_tokens(const Kv& kv, const KvBatch& batch, const Query& q, ui
     const bool one = most_rows <= 8;
     auto* kernel = one ? token_attention_kernel<T, kDim, 1> : token_attention_kernel<T, kDim, 2>;
     const uint32_t smem = kTokenWarps * kTokenStageBytes<kDim> * (one ? kTokenStages<kDim, 1> : kTokenStages<kDim, 2>);
-    static_assert(kTokenStageBytes<kDim> * kTokenStages<kDim, 1> >= 8u * (kDim + 4u) * 4u &&
-                      kTokenStageBytes<kDim> * kTokenStages<kDim, 2> >= 16u * (kDim + 4u) * 4u,
-                  "the joined sums fit where the rings were");
-    if (smem > 48u * 1024u) {        // per device, so not remembered here
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
-    const uint32_t blocks = min(kTokenBlocks, (one ? 2u : 1u) * sm_count);
-    kernel<<<blocks, kTokenThreads, smem, s>>>(kv, batch, q, partials);
+    static std::atomic<uint64_t> allowed[2];         // bit per device: the kernel may use that much shared memory there
+    if (cudaError_t e = allow_shared((const void*)kernel, smem, allowed[one])) return e;
+    kernel<<<(one ? 2u : 1u) * sm_count, kTokenThreads, smem, s>>>(kv, batch, q, partials, most_rows);
     return cudaGetLastError();
 }
 
