@@ -527,14 +527,16 @@ __global__ void __launch_bounds__(kTokenThreads, kTiles == 1 ? 2 : 1)
             const uint32_t count = min(kJoin, (many - first_of + span8 - 1u) / span8);
             const bool top_level = count * span8 >= many;            // then first_of is 0
             if (count > 1u) {
-                __threadfence();
                 __syncwarp();
                 uint32_t before = 0;
                 uint32_t* arrived = &kv.head->token_arrived[level][c0 + first_of];
-                if (lane == 0) before = atomicAdd(arrived, 1u);
+                if (lane == 0) {             // behind the barrier the lane's fences stand for the whole warp's writes and reads
+                    __threadfence();
+                    before = atomicAdd(arrived, 1u);
+                    __threadfence();
+                }
                 if (__shfl_sync(0xffffffffu, before, 0) != count - 1u) break;
                 if (lane == 0) *arrived = 0u;
-                __threadfence();
                 // share c0's result lies in its second place, those of the others in their first
                 auto result = [&](uint32_t i) {
                     const uint32_t c = first_of + i * span8;
