@@ -98,9 +98,40 @@ inline entro_status kv_check(const entro_kv_cache* c, const entro_kv_batch* b, K
     return ENTRO_OK;
 }
 
+// Launches a kernel so that it may be set up while the kernel before it in the stream ends; dependent_start() in the
+// kernel then waits for that end (and for its writes).  Between the short kernels of a token step this hides most of
+// the launch.
+template <typename... Params, typename... Args>
+cudaError_t launch_dependent_shared(void (*kernel)(Params...), dim3 grid, uint32_t threads, uint32_t shared, cudaStream_t s,
+                                    const Args&... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+template <typename... Params, typename... Args>
+cudaError_t launch_dependent(void (*kernel)(Params...), dim3 grid, uint32_t threads, cudaStream_t s, const Args&... args)
+{
+    return launch_dependent_shared(kernel, grid, threads, 0u, s, args...);
+}
+
 inline bool kv_strides_ok(int64_t row, int64_t head) { return row % 8 == 0 && head % 8 == 0; }
 
 namespace {
+
+// First thing in a kernel of launch_dependent: lets the next kernel be set up, waits for the one before.
+__device__ __forceinline__ void dependent_start()
+{
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+}
 
 // Page of block `block` of a slot, or -1.
 __device__ __forceinline__ int kv_page(const Kv& kv, int slot, uint32_t block)

@@ -1,8 +1,8 @@
 // Page operations of the key/value cache: reserve, fork, free, trim, compact.
 //
-// Each is planned by ONE cluster of eight CTAs (8192 threads): the work is counters and small
-// tables, bound by latency, and a cluster has a hardware barrier and a shared view of memory, so
-// all phases fit in one launch with no host in between.  What has to be copied (fork: the pages
+// Each is planned in ONE launch, by a block of 1024 threads or, where there is much to go through, by
+// a cluster of eight: the work is counters and small tables, bound by latency, and a cluster has a
+// hardware barrier and a shared view of memory, so no host and no second launch come in between.  What has to be copied (fork: the pages
 // that are not full; compact: the pages that move) is left as a list of pairs in the work area for
 // copy_pages_kernel, which spreads it over the whole GPU.
 #include "entro_kv_common.cuh"
@@ -10,10 +10,17 @@
 namespace entro {
 namespace {
 
-constexpr uint32_t kPlanCtas = 8, kPlanThreads = 1024;
+// Above this many table entries and pages eight blocks are quicker than one (a barrier between blocks costs about 0.7 us, one
+// inside a block next to nothing).
+constexpr uint64_t kPlanOne = 16384;
+constexpr uint32_t kPlanMost = 8, kPlanThreads = 1024;
 
-__device__ __forceinline__ void cluster_barrier()
+__device__ __forceinline__ void plan_barrier()
 {
+    if (gridDim.x == 1u) {
+        __syncthreads();
+        return;
+    }
     // release / acquire at cluster scope: what the CTAs wrote to global memory before is visible after
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -48,7 +55,7 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* total)
 // Pages [lo, hi) of this CTA of the planning cluster.
 __device__ __forceinline__ void segment(uint32_t pages, uint32_t* lo, uint32_t* hi)
 {
-    const uint32_t each = (pages + kPlanCtas - 1u) / kPlanCtas;
+    const uint32_t each = (pages + gridDim.x - 1u) / gridDim.x;
     *lo = min(pages, blockIdx.x * each);
     *hi = min(pages, *lo + each);
 }
@@ -77,20 +84,20 @@ __device__ __forceinline__ void rank_pages(uint32_t lo, uint32_t hi, uint32_t ra
     }
 }
 
-// part[offset .. + kPlanCtas) holds one count per CTA: the sum before this CTA and the sum of all.
+// part[offset .. + blocks) holds one count per CTA: the sum before this CTA and the sum of all.
 __device__ __forceinline__ void part_sums(const uint32_t* part, uint32_t* before, uint32_t* all)
 {
     *before = *all = 0;
 #pragma unroll
-    for (uint32_t c = 0; c < kPlanCtas; ++c) {
-        const uint32_t v = __ldcg(part + c);
+    for (uint32_t c = 0; c < kPlanMost; ++c) {
+        const uint32_t v = c < gridDim.x ? __ldcg(part + c) : 0u;
         *before += c < blockIdx.x ? v : 0u;
         *all += v;
     }
 }
 
 // The `want` lowest free pages in ascending order into fresh[]; returns how many there are.  The
-// caller has a cluster barrier before (counts final) and one after (fresh[] and refs in place).
+// caller has a barrier before (counts final) and one after (fresh[] and refs in place).
 __device__ __forceinline__ uint32_t take_lowest_free(const Kv& kv, uint32_t want, int32_t* fresh, uint32_t* part)
 {
     uint32_t lo, hi, before, all;
@@ -98,7 +105,7 @@ __device__ __forceinline__ uint32_t take_lowest_free(const Kv& kv, uint32_t want
     auto is_free = [&](uint32_t p) { return __ldcg(kv.refs + p) <= 0; };
     const uint32_t mine = count_pages(lo, hi, is_free);
     if (threadIdx.x == 0) part[blockIdx.x] = mine;
-    cluster_barrier();
+    plan_barrier();
     part_sums(part, &before, &all);
     rank_pages(lo, hi, before, want, is_free, [&](uint32_t rank, uint32_t p) {
         fresh[rank] = (int32_t)p;
@@ -116,6 +123,7 @@ __device__ __forceinline__ uint32_t blocks_of(const Kv& kv, int len)
 
 __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Kv kv, KvBatch batch)
 {
+    dependent_start();
     // offs[b]: pages needed by the sequences before b
     uint32_t* offs = (uint32_t*)kv.region;
     int32_t* fresh = (int32_t*)(offs + kv.slots);
@@ -138,9 +146,9 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Kv kv, KvBatch ba
     }
     const uint32_t got = take_lowest_free(kv, want, fresh, kv.head->part);
     if (blockIdx.x == 0 && (full_row || (got < want && threadIdx.x == 0))) atomicOr(&kv.head->status, kKvStatNoPages);
-    cluster_barrier();
+    plan_barrier();
     const uint32_t lane = threadIdx.x & 31u;
-    for (uint32_t b = plan_rank() >> 5; b < batch.n; b += kPlanCtas * kPlanThreads / 32u) {
+    for (uint32_t b = plan_rank() >> 5; b < batch.n; b += gridDim.x * kPlanThreads / 32u) {
         const int slot = batch.slot(b, kv.slots);
         if (slot < 0) continue;
         const int len = __ldcg(kv.lens + slot), rows = batch.count(b);
@@ -159,13 +167,14 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Kv kv, KvBatch ba
 // Rows of the new tables wait in the region ([n][width]) until every src has been read.
 __global__ void __launch_bounds__(kPlanThreads) fork_kernel(Kv kv, const int32_t* src, const int32_t* dst, uint32_t n)
 {
+    dependent_start();
     int32_t* rows = (int32_t*)kv.region;
     int32_t* new_len = rows + (uint64_t)kv.slots * kv.width;
     int32_t* fresh = new_len + kv.slots;
     int32_t* tail = fresh + kv.slots;         // [n] page that is copied for pair i, -1: none
     int32_t* pair_from = tail + kv.slots;
     int32_t* pair_to = pair_from + kv.pages;
-    const uint32_t lane = threadIdx.x & 31u, warps = kPlanCtas * kPlanThreads / 32u;
+    const uint32_t lane = threadIdx.x & 31u, warps = gridDim.x * kPlanThreads / 32u;
     auto live = [&](uint32_t i, int* s, int* d) {
         *s = __ldg(src + i);
         *d = __ldg(dst + i);
@@ -192,7 +201,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_kernel(Kv kv, const int32_t
             new_len[i] = len;
         }
     }
-    cluster_barrier();
+    plan_barrier();
     // what the targets held is released
     for (uint32_t i = plan_rank() >> 5; i < n; i += warps) {
         int s, d;
@@ -210,9 +219,9 @@ __global__ void __launch_bounds__(kPlanThreads) fork_kernel(Kv kv, const int32_t
         block_scan(i < n && __ldcg(tail + i) >= 0, &total);
         want += total;
     }
-    cluster_barrier();
+    plan_barrier();
     const uint32_t got = take_lowest_free(kv, want, fresh, kv.head->part);
-    cluster_barrier();
+    plan_barrier();
     // pairs in the order of i; the held tail pages are let go
     if (blockIdx.x == 0) {
         uint32_t at0 = 0;
@@ -237,7 +246,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_kernel(Kv kv, const int32_t
             if (got < want) atomicOr(&kv.head->status, kKvStatNoPages);
         }
     }
-    cluster_barrier();
+    plan_barrier();
     for (uint32_t i = plan_rank() >> 5; i < n; i += warps) {
         int s, d;
         if (!live(i, &s, &d)) continue;
@@ -254,6 +263,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_kernel(Kv kv, const int32_t
 __global__ void __launch_bounds__(256) release_kernel(Kv kv, const int32_t* slots, uint32_t n, bool trim, uint32_t window,
                                                       uint32_t sinks)
 {
+    dependent_start();
     const uint32_t i = (blockIdx.x * 256u + threadIdx.x) >> 5, lane = threadIdx.x & 31u;
     if (i >= n) return;
     const int slot = __ldg(slots + i);
@@ -279,6 +289,7 @@ __global__ void __launch_bounds__(256) release_kernel(Kv kv, const int32_t* slot
 
 __global__ void __launch_bounds__(kPlanThreads) compact_kernel(Kv kv)
 {
+    dependent_start();
     int32_t* from = (int32_t*)kv.region;      // [pages] pages that move, ascending
     int32_t* to = from + kv.pages;            // [pages] free places that they go to, ascending
     int32_t* moved = to + kv.pages;           // [pages] new place of a page
@@ -288,33 +299,33 @@ __global__ void __launch_bounds__(kPlanThreads) compact_kernel(Kv kv)
     const uint32_t mine = count_pages(lo, hi, is_live);
     uint32_t* part = kv.head->part;
     if (threadIdx.x == 0) part[blockIdx.x] = mine;
-    cluster_barrier();
+    plan_barrier();
     part_sums(part, &before, &live);
     const uint32_t low_hi = min(hi, max(lo, live)), high_lo = max(lo, min(hi, live));
     const uint32_t free_low = (low_hi - lo) - count_pages(lo, low_hi, is_live);
     const uint32_t live_high = count_pages(high_lo, hi, is_live);
     if (threadIdx.x == 0) {
-        part[kPlanCtas + blockIdx.x] = free_low;
-        part[2 * kPlanCtas + blockIdx.x] = live_high;
+        part[kPlanMost + blockIdx.x] = free_low;
+        part[2 * kPlanMost + blockIdx.x] = live_high;
     }
-    cluster_barrier();
-    part_sums(part + kPlanCtas, &holes_before, &holes);
-    part_sums(part + 2 * kPlanCtas, &movers_before, &movers);
+    plan_barrier();
+    part_sums(part + kPlanMost, &holes_before, &holes);
+    part_sums(part + 2 * kPlanMost, &movers_before, &movers);
     rank_pages(lo, low_hi, holes_before, holes, [&](uint32_t p) { return !is_live(p); },
                [&](uint32_t rank, uint32_t p) { to[rank] = (int32_t)p; });
     rank_pages(high_lo, hi, movers_before, movers, is_live, [&](uint32_t rank, uint32_t p) { from[rank] = (int32_t)p; });
-    cluster_barrier();
-    for (uint32_t k = plan_rank(); k < movers; k += kPlanCtas * kPlanThreads) {
+    plan_barrier();
+    for (uint32_t k = plan_rank(); k < movers; k += gridDim.x * kPlanThreads) {
         const int f = __ldcg(from + k), t = __ldcg(to + k);
         kv.refs[t] = __ldcg(kv.refs + f);
         kv.refs[f] = 0;
         moved[f] = t;
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) kv.head->pairs = movers;
-    cluster_barrier();
+    plan_barrier();
     if (movers == 0) return;
     const uint32_t lane = threadIdx.x & 31u;
-    for (uint32_t s = plan_rank() >> 5; s < kv.slots; s += kPlanCtas * kPlanThreads / 32u) {
+    for (uint32_t s = plan_rank() >> 5; s < kv.slots; s += gridDim.x * kPlanThreads / 32u) {
         const uint32_t used = blocks_of(kv, __ldg(kv.lens + s));
         for (uint32_t e = lane; e < used; e += 32u) {
             int32_t* at = kv.table + (uint64_t)s * kv.width + e;
@@ -332,6 +343,7 @@ constexpr uint32_t kCopyPiece = 16384;
 
 __global__ void __launch_bounds__(256) copy_pages_kernel(Kv kv, const int32_t* from, const int32_t* to)
 {
+    dependent_start();
     const uint32_t pairs = __ldcg(&kv.head->pairs);
     const uint32_t page_bytes = (uint32_t)kv.page_bytes(), pieces = (page_bytes + kCopyPiece - 1u) / kCopyPiece;
     const uint64_t all = (uint64_t)pairs * pieces;
@@ -354,20 +366,24 @@ __global__ void __launch_bounds__(256) copy_pages_kernel(Kv kv, const int32_t* f
     }
 }
 
-template <typename... Args>
-cudaError_t launch_plan(void (*kernel)(Args...), cudaStream_t s, Args... args)
+// `work`: table entries and pages that the plan goes through.
+template <typename... Params, typename... Args>
+cudaError_t launch_plan(void (*kernel)(Params...), uint64_t work, cudaStream_t s, const Args&... args)
 {
+    const uint32_t blocks = work <= kPlanOne ? 1u : kPlanMost;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kPlanCtas);
+    cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(kPlanThreads);
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = kPlanCtas;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = blocks;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
@@ -381,9 +397,8 @@ entro_status launch_copy(const Kv& kv, const int32_t* from, const int32_t* to, u
     if (!ws) return ENTRO_ERR_CUDA;
     const uint64_t pieces = most_pairs * ((kv.page_bytes() + kCopyPiece - 1) / kCopyPiece);
     const uint64_t most = (uint64_t)ws->sm_count * 8u;
-    copy_pages_kernel<<<(unsigned)(pieces < most ? pieces : most), 256, 0, s>>>(kv, from, to);
+    ENTRO_CUDA(launch_dependent(copy_pages_kernel, dim3((unsigned)(pieces < most ? pieces : most)), 256u, s, kv, from, to));
     count_launch(2);
-    ENTRO_CUDA(cudaGetLastError());
     return ENTRO_OK;
 }
 
@@ -416,7 +431,7 @@ extern "C" entro_status entro_kv_reserve(const entro_kv_cache* cache, const entr
     if (entro_status e = kv_check(cache, &kv)) return e;
     if (entro_status e = kv_check(cache, b, &batch)) return e;
     if (batch.n == 0 || batch.rows == 0) return ENTRO_OK;
-    ENTRO_CUDA(launch_plan(reserve_kernel, (cudaStream_t)cuda_stream, kv, batch));
+    ENTRO_CUDA(launch_plan(reserve_kernel, kv.pages, (cudaStream_t)cuda_stream, kv, batch));
     count_launch();
     return ENTRO_OK;
 }
@@ -428,7 +443,7 @@ extern "C" entro_status entro_kv_fork(const entro_kv_cache* cache, const int32_t
     if (entro_status e = kv_check(cache, &kv)) return e;
     if (n == 0) return ENTRO_OK;
     if (!src || !dst || !aligned(src, 4) || !aligned(dst, 4) || n > kv.slots) return ENTRO_ERR_INVALID_ARG;
-    ENTRO_CUDA(launch_plan(fork_kernel, (cudaStream_t)cuda_stream, kv, src, dst, n));
+    ENTRO_CUDA(launch_plan(fork_kernel, (uint64_t)n * kv.width + kv.pages, (cudaStream_t)cuda_stream, kv, src, dst, n));
     const int32_t* from = (const int32_t*)kv.region + (uint64_t)kv.slots * kv.width + 3ull * kv.slots;
     return launch_copy(kv, from, from + kv.pages, n, (cudaStream_t)cuda_stream);
 }
@@ -439,9 +454,8 @@ extern "C" entro_status entro_kv_free(const entro_kv_cache* cache, const int32_t
     if (entro_status e = kv_check(cache, &kv)) return e;
     if (n == 0) return ENTRO_OK;
     if (!slots || !aligned(slots, 4) || n > kv.slots) return ENTRO_ERR_INVALID_ARG;
-    release_kernel<<<(n + 7u) / 8u, 256, 0, (cudaStream_t)cuda_stream>>>(kv, slots, n, false, 0u, 0u);
+    ENTRO_CUDA(launch_dependent(release_kernel, dim3((n + 7u) / 8u), 256u, (cudaStream_t)cuda_stream, kv, slots, n, false, 0u, 0u));
     count_launch();
-    ENTRO_CUDA(cudaGetLastError());
     return ENTRO_OK;
 }
 
@@ -452,9 +466,8 @@ extern "C" entro_status entro_kv_trim(const entro_kv_cache* cache, const int32_t
     if (entro_status e = kv_check(cache, &kv)) return e;
     if (n == 0 || window == 0) return ENTRO_OK;
     if (!slots || !aligned(slots, 4) || n > kv.slots) return ENTRO_ERR_INVALID_ARG;
-    release_kernel<<<(n + 7u) / 8u, 256, 0, (cudaStream_t)cuda_stream>>>(kv, slots, n, true, window, sinks);
+    ENTRO_CUDA(launch_dependent(release_kernel, dim3((n + 7u) / 8u), 256u, (cudaStream_t)cuda_stream, kv, slots, n, true, window, sinks));
     count_launch();
-    ENTRO_CUDA(cudaGetLastError());
     return ENTRO_OK;
 }
 
@@ -462,7 +475,7 @@ extern "C" entro_status entro_kv_compact(const entro_kv_cache* cache, void* cuda
 {
     Kv kv;
     if (entro_status e = kv_check(cache, &kv)) return e;
-    ENTRO_CUDA(launch_plan(compact_kernel, (cudaStream_t)cuda_stream, kv));
+    ENTRO_CUDA(launch_plan(compact_kernel, (uint64_t)kv.slots * kv.width + kv.pages, (cudaStream_t)cuda_stream, kv));
     const int32_t* from = (const int32_t*)kv.region;
     return launch_copy(kv, from, from + kv.pages, kv.pages / 2u + 1u, (cudaStream_t)cuda_stream);
 }

@@ -334,6 +334,7 @@ template <typename T, int kDim>
 __global__ void __launch_bounds__(kPromptThreads, 1)
     prompt_attention_kernel(Kv kv, KvBatch batch, Query q, float* partials, uint32_t few_rows)
 {
+    dependent_start();
     constexpr uint32_t kTile = kPromptSlabs<kDim> * kSlabBytes;
     extern __shared__ __align__(1024) unsigned char tiles[];
     unsigned char* const k_tile = tiles + 3 * kTile;         // [2] stages; the three Q tiles come first
@@ -1009,8 +1010,8 @@ cudaError_t launch_prompt(const Kv& kv, const KvBatch& batch, const Query& q, ui
     auto* kernel = prompt_attention_kernel<T, kDim>;
     static std::atomic<uint64_t> allowed;
     if (cudaError_t e = allow_shared((const void*)kernel, kPromptSmem<kDim>, allowed)) return e;
-    kernel<<<min(kPromptBlocks, sm_count), kPromptThreads, kPromptSmem<kDim>, s>>>(kv, batch, q, partials, few_rows);
-    return cudaGetLastError();
+    return launch_dependent_shared(kernel, dim3(min(kPromptBlocks, sm_count)), kPromptThreads, kPromptSmem<kDim>, s, kv, batch, q, partials,
+                                   few_rows);
 }
 
 }  // namespace

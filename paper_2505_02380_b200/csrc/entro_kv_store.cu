@@ -9,6 +9,11 @@ constexpr float kScaleFloor = 8.673617379884035e-19f;   // 2^-60: no scale is 0,
 struct Rows {
     const unsigned char* base[2];   // keys, values
     int64_t row[2], head[2];        // strides in bytes
+    // (selected, not indexed: an index that is not a constant would put the arguments into local memory)
+    __device__ __forceinline__ const unsigned char* at(uint32_t which, int64_t r, uint32_t h) const
+    {
+        return which ? base[1] + r * row[1] + h * head[1] : base[0] + r * row[0] + h * head[0];
+    }
 };
 
 // Work items of a ragged batch: sequence b's touched pages are items f(b) + 0, 1, ... with
@@ -54,123 +59,218 @@ __device__ __forceinline__ Item find_item(const Kv& kv, const KvBatch& batch, ui
     return it;
 }
 
-// One block per (touched page, head, keys or values).  Bound by memory: a new value is read once
-// (2 bytes) and written once (1 byte); it waits in registers for the page's maximum.  Old tokens
-// of the page are only touched when its scale grows.
-template <typename T, int kVec>
-__global__ void __launch_bounds__(256) append_kernel(Kv kv, KvBatch batch, Rows rows)
-{
-    const Item it = find_item(kv, batch, blockIdx.x);
-    const uint32_t head = blockIdx.y, which = blockIdx.z;
-    if (it.page < 0) return;
-    const uint32_t per_token = kv.dim / 8u;
-    uint8_t* codes = kv.codes + (uint64_t)it.page * kv.page_bytes() + (which * kv.heads + head) * kv.head_bytes();
-    float* scale_at = kv.scales + ((uint64_t)it.page * 2u + which) * kv.heads + head;
-    const float old_scale = it.lo ? *scale_at : 0.f;
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }     // false for infinities and NaN
 
-    uint4 x[kVec];
+// Largest magnitude of eight values, without those that are not finite; `odd` is set where there are any.
+template <typename T>
+__device__ __forceinline__ float largest(const uint4& x, bool& odd)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     float top = 0.f;
-    bool odd = false;
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-        const uint32_t i = threadIdx.x + 256u * j, token = i / per_token, part = i - token * per_token;
-        x[j] = make_uint4(0u, 0u, 0u, 0u);
-        if (token >= it.lo && token < it.hi) {
-            const int64_t row = it.row0 + (int)(token - it.lo);
-            x[j] = __ldg((const uint4*)(rows.base[which] + row * rows.row[which] + head * rows.head[which]) + part);
-        }
+    for (int e = 0; e < 4; ++e) {
+        const float2 f = to_float2<T>(w[e]);
+        const bool fa = finite(f.x), fb = finite(f.y);
+        top = fmaxf(top, fmaxf(fa ? fabsf(f.x) : 0.f, fb ? fabsf(f.y) : 0.f));
+        odd |= !(fa && fb);
     }
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-        const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float2 f = to_float2<T>(w[e]);
-            const float a = fabsf(f.x), b = fabsf(f.y);
-            const bool fa = a <= 3.402823466e38f, fb = b <= 3.402823466e38f;   // false for infinities and NaN
-            top = fmaxf(top, fmaxf(fa ? a : 0.f, fb ? b : 0.f));
-            odd |= !(fa && fb);
-        }
-    }
-#pragma unroll
-    for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-    __shared__ float tops[8];
-    if ((threadIdx.x & 31u) == 0) tops[threadIdx.x >> 5] = top;
-    if (__syncthreads_or(odd) && threadIdx.x == 0) atomicOr(&kv.head->status, kKvStatNonfinite);
-#pragma unroll
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, tops[w]);
-    const float scale = fmaxf(fmaxf(old_scale, __fdiv_rn(top, 127.f)), kScaleFloor);
-    const bool grown = it.lo && scale != old_scale;
-    const float ratio = __fdiv_rn(old_scale, scale);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-        const uint32_t i = threadIdx.x + 256u * j, token = i / per_token;
-        uint2* at = (uint2*)codes + i;
-        if (token >= it.lo && token < it.hi) {
-            const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-            uint32_t out[2] = {0u, 0u};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 f = to_float2<T>(w[e]);
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const float v = p ? f.y : f.x;
-                    // an infinity divides to an infinity and is clamped; the maximum is finite, so no NaN arises from it
-                    float q = rintf(__fdiv_rn(v, scale));
-                    q = v == v ? fminf(fmaxf(q, -127.f), 127.f) : 0.f;
-                    out[e >> 1] |= (uint32_t)((int)q + ENTRO_KV_ZERO_POINT) << (16 * (e & 1) + 8 * p);
-                }
-            }
-            *at = make_uint2(out[0], out[1]);
-        } else if (grown && token < it.lo) {
-            const uint2 old = *at;
-            const uint32_t w[2] = {old.x, old.y};
-            uint32_t out[2] = {0u, 0u};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float q = (float)((int)(w[e >> 2] >> (8 * (e & 3)) & 0xffu) - ENTRO_KV_ZERO_POINT);
-                const float r = fminf(fmaxf(rintf(__fmul_rn(q, ratio)), -128.f), 127.f);
-                out[e >> 2] |= (uint32_t)((int)r + ENTRO_KV_ZERO_POINT) << (8 * (e & 3));
-            }
-            *at = make_uint2(out[0], out[1]);
-        }
-    }
-    if (threadIdx.x == 0) *scale_at = scale;
+    return top;
 }
 
-// One block per row; a thread takes eight values at a time.
+// rne(x / scale) + 128 of eight values.  The quotient by way of the reciprocal is off by less than 127 * 2^-22; only where
+// it lies that near the middle between two codes (one value in 10^4) the division itself decides.  Adding 1.5 * 2^23 + 128
+// rounds to nearest even and leaves the code in the lowest byte.
+template <typename T>
+__device__ __forceinline__ uint2 quantise(const uint4& x, float scale, float inverse, bool odd)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t out[2];
+    constexpr float kPlace = 12582912.f + ENTRO_KV_ZERO_POINT;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float z[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 f = to_float2<T>(w[2 * h + (e >> 1)]);
+            const float v = e & 1 ? f.y : f.x, y = __fmul_rn(v, inverse);
+            z[e] = __fadd_rn(y, kPlace);
+            const float off = fabsf(__fadd_rn(y, -__fadd_rn(z[e], -kPlace)));
+            if (odd || off > 0.4999f) {
+                const float q = rintf(__fdiv_rn(v, scale));
+                z[e] = kPlace + (v == v ? fminf(fmaxf(q, -127.f), 127.f) : 0.f);
+            }
+        }
+        const uint32_t lo = __byte_perm(__float_as_uint(z[0]), __float_as_uint(z[1]), 0x0040);
+        const uint32_t hi = __byte_perm(__float_as_uint(z[2]), __float_as_uint(z[3]), 0x0040);
+        out[h] = __byte_perm(lo, hi, 0x5410);
+    }
+    return make_uint2(out[0], out[1]);
+}
+
+// Eight old codes of a page whose scale has grown.
+__device__ __forceinline__ uint2 requantise(const uint2& old, float ratio)
+{
+    const uint32_t w[2] = {old.x, old.y};
+    uint32_t out[2] = {0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float q = (float)((int)(w[e >> 2] >> (8 * (e & 3)) & 0xffu) - ENTRO_KV_ZERO_POINT);
+        const float r = fminf(fmaxf(rintf(__fmul_rn(q, ratio)), -128.f), 127.f);
+        out[e >> 2] |= (uint32_t)((int)r + ENTRO_KV_ZERO_POINT) << (8 * (e & 3));
+    }
+    return make_uint2(out[0], out[1]);
+}
+
+// One new row per sequence: a warp per (sequence, head, keys or values).  What counts is latency: lengths, table, scale,
+// one after the other; the row is fetched meanwhile.  The page's old codes are touched only when its scale grows.
+template <typename T>
+__global__ void __launch_bounds__(256) append_one_kernel(Kv kv, KvBatch batch, Rows rows)
+{
+    dependent_start();
+    const uint32_t lane = threadIdx.x & 31u, unit = blockIdx.x * 8u + (threadIdx.x >> 5), per_token = kv.dim / 8u;
+    if (unit >= batch.n * kv.heads * 2u) return;
+    const uint32_t b = unit / (kv.heads * 2u), rest = unit - b * kv.heads * 2u, which = rest >= kv.heads, head = rest - which * kv.heads;
+    uint4 x = make_uint4(0u, 0u, 0u, 0u);
+    if (lane < per_token) x = __ldg((const uint4*)rows.at(which, b, head) + lane);
+    const int slot = batch.slot(b, kv.slots);
+    if (slot < 0) return;
+    const int position = __ldg(kv.lens + slot) - 1;
+    if (position < 0) return;
+    const int page = kv_page(kv, slot, (uint32_t)position >> kv.page_shift);
+    if (page < 0) return;
+    const uint32_t token = (uint32_t)position & (kv.page() - 1u);
+    uint2* codes = (uint2*)(kv.codes + (uint64_t)page * kv.page_bytes() + (which * kv.heads + head) * kv.head_bytes());
+    float* scale_at = kv.scales + ((uint64_t)page * 2u + which) * kv.heads + head;
+    const float old_scale = token ? *scale_at : 0.f;
+    bool odd = false;
+    float top = largest<T>(x, odd);
+#pragma unroll
+    for (int s = 8; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+    odd = __any_sync(0xffffffffu, odd);
+    if (odd && lane == 0) atomicOr(&kv.head->status, kKvStatNonfinite);
+    const float scale = __shfl_sync(0xffffffffu, fmaxf(fmaxf(old_scale, __fdiv_rn(top, 127.f)), kScaleFloor), 0);
+    if (token && scale != old_scale) {
+        const float ratio = __fdiv_rn(old_scale, scale);
+#pragma unroll 4
+        for (uint32_t i = lane; i < token * per_token; i += 32u) codes[i] = requantise(codes[i], ratio);
+    }
+    if (lane < per_token) codes[token * per_token + lane] = quantise<T>(x, scale, __frcp_rn(scale), odd);
+    if (lane == 0) *scale_at = scale;
+}
+
+// Any number of new rows: a block per touched page and `per_block` of its heads (keys and values apart).  Bound by memory:
+// a new value is read once (2 bytes) and written once (1 byte); it waits in registers for the page's maximum, while the
+// next head's values are on their way.
+template <typename T, int kVec>
+__global__ void __launch_bounds__(256) append_kernel(Kv kv, KvBatch batch, Rows rows, uint32_t per_block)
+{
+    dependent_start();
+    const Item it = find_item(kv, batch, blockIdx.x);
+    if (it.page < 0) return;
+    __shared__ float tops[2][8];
+    const uint32_t per_token = kv.dim / 8u, sides = 2u * kv.heads;
+    const uint32_t begin = blockIdx.y * per_block, end = min(sides, begin + per_block);
+    uint32_t token[kVec], part[kVec];
+    bool fresh[kVec];
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+        const uint32_t i = threadIdx.x + 256u * j;
+        token[j] = i / per_token;
+        part[j] = i - token[j] * per_token;
+        fresh[j] = token[j] >= it.lo && token[j] < it.hi;
+    }
+    auto load = [&](uint32_t side, uint4(&x)[kVec]) {
+        const uint32_t which = side >= kv.heads, head = side - which * kv.heads;
+        const unsigned char* base = rows.at(which, it.row0 - (int)it.lo, head);
+        const int64_t stride = which ? rows.row[1] : rows.row[0];
+#pragma unroll
+        for (int j = 0; j < kVec; ++j)
+            x[j] = fresh[j] ? __ldcs((const uint4*)(base + (int64_t)token[j] * stride) + part[j])
+                            : make_uint4(0u, 0u, 0u, 0u);
+    };
+    uint4 x[kVec], next[kVec];
+    load(begin, x);
+    for (uint32_t side = begin; side < end; ++side) {
+        float* scale_at = kv.scales + (uint64_t)it.page * sides + side;
+        const float old_scale = it.lo ? *scale_at : 0.f;
+        if (side + 1u < end) load(side + 1u, next);
+        bool odd = false;
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) top = fmaxf(top, largest<T>(x[j], odd));
+#pragma unroll
+        for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+        float* mine = tops[side & 1u];           // the other half is still being read for the side before
+        if ((threadIdx.x & 31u) == 0) mine[threadIdx.x >> 5] = top;
+        odd = __syncthreads_or(odd);
+        if (odd && threadIdx.x == 0) atomicOr(&kv.head->status, kKvStatNonfinite);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) top = fmaxf(top, mine[w]);
+        const float scale = fmaxf(fmaxf(old_scale, __fdiv_rn(top, 127.f)), kScaleFloor), inverse = __frcp_rn(scale);
+        const bool grown = it.lo && scale != old_scale;
+        uint2* codes = (uint2*)(kv.codes + (uint64_t)it.page * kv.page_bytes() + side * kv.head_bytes());
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+            uint2* at = codes + threadIdx.x + 256u * j;
+            if (fresh[j])
+                *at = quantise<T>(x[j], scale, inverse, odd);
+            else if (grown && token[j] < it.lo)
+                *at = requantise(*at, __fdiv_rn(old_scale, scale));
+        }
+        // every thread has read the old scale before the barrier above
+        if (threadIdx.x == 0) *scale_at = scale;
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) x[j] = next[j];
+    }
+}
+
+// A warp per row; a lane takes sixteen values at a time.
 template <typename T>
 __global__ void __launch_bounds__(256) read_kernel(Kv kv, KvBatch batch, Rows rows)
 {
-    const uint32_t row = blockIdx.x;
-    int b = (int)row;
+    dependent_start();
+    const uint32_t lane = threadIdx.x & 31u, row = blockIdx.x * 8u + (threadIdx.x >> 5);
+    if (row >= batch.rows) return;
+    uint32_t b = row;
     if (batch.row_start) {
-        b = block_find(batch.n, row, [&](uint32_t i) { return (uint32_t)batch.first(i); });
-        if (b < 0 || (int)row >= batch.first(b) + batch.count(b)) return;
+        // the last sequence that begins at or before the row, by a search with 32 probes at a time
+        b = 0;
+        for (uint32_t left = batch.n; left > 1u;) {
+            const uint32_t stride = (left + 31u) / 32u;
+            const uint32_t in = __ballot_sync(0xffffffffu, lane * stride < left && (uint32_t)batch.first(min(b + lane * stride, batch.n - 1u)) <= row);
+            const uint32_t k = in ? 31u - __clz(in) : 0u;
+            b += k * stride;
+            left = min(stride, left - k * stride);
+        }
+        if ((int)row < batch.first(b) || (int)row >= batch.first(b) + batch.count(b)) return;
     }
     const int slot = batch.slot(b, kv.slots);
     const int len = slot >= 0 ? __ldg(kv.lens + slot) : 0;
     const int position = len - batch.count(b) + ((int)row - batch.first(b));
     const int page = position >= 0 && slot >= 0 ? kv_page(kv, slot, (uint32_t)position >> kv.page_shift) : -1;
-    const uint32_t token = (uint32_t)position & (kv.page() - 1u), per_token = kv.dim / 8u, per_side = kv.heads * per_token;
-    for (uint32_t i = threadIdx.x; i < 2u * per_side; i += blockDim.x) {
-        const uint32_t which = i >= per_side, head = (i - which * per_side) / per_token, part = i - which * per_side - head * per_token;
-        uint4 out = make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t token = (uint32_t)position & (kv.page() - 1u), per_token = kv.dim / 16u, per_side = kv.heads * per_token;
+#pragma unroll 4
+    for (uint32_t i = lane; i < 2u * per_side; i += 32u) {
+        const uint32_t which = i >= per_side, at = i - which * per_side, head = at / per_token, part = at - head * per_token;
+        uint4 out[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
         if (page >= 0) {
             const uint8_t* codes = kv.codes + (uint64_t)page * kv.page_bytes() + (which * kv.heads + head) * kv.head_bytes();
-            const uint2 c = __ldg((const uint2*)codes + token * per_token + part);
+            const uint4 c = __ldcs((const uint4*)(codes + token * kv.dim) + part);
             const float s = __ldg(kv.scales + ((uint64_t)page * 2u + which) * kv.heads + head);
-            const uint32_t w[2] = {c.x, c.y};
-            uint32_t o[4];
+            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+            uint32_t o[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < 8; ++e) {
                 const uint32_t two = w[e >> 1] >> (16 * (e & 1));
                 o[e] = from_float2<T>(__fmul_rn(s, (float)((int)(two & 0xffu) - ENTRO_KV_ZERO_POINT)),
                                       __fmul_rn(s, (float)((int)(two >> 8 & 0xffu) - ENTRO_KV_ZERO_POINT)));
             }
-            out = make_uint4(o[0], o[1], o[2], o[3]);
+            out[0] = make_uint4(o[0], o[1], o[2], o[3]);
+            out[1] = make_uint4(o[4], o[5], o[6], o[7]);
         }
-        *((uint4*)(const_cast<unsigned char*>(rows.base[which]) + (int64_t)row * rows.row[which] + head * rows.head[which]) + part) = out;
+        uint4* to = (uint4*)const_cast<unsigned char*>(rows.at(which, row, head)) + 2u * part;
+        __stcs(to, out[0]);
+        __stcs(to + 1, out[1]);
     }
 }
 
@@ -188,17 +288,21 @@ entro_status check_rows(const entro_kv_rows* r, Rows* out)
 }
 
 template <typename T>
-void launch_append(const Kv& kv, const KvBatch& batch, const Rows& rows, dim3 grid, cudaStream_t s)
+cudaError_t launch_append(const Kv& kv, const KvBatch& batch, const Rows& rows, cudaStream_t s)
 {
-    const uint32_t vectors = kv.page() * kv.dim / 8u;
-    if (vectors <= 256u)
-        append_kernel<T, 1><<<grid, 256, 0, s>>>(kv, batch, rows);
-    else if (vectors <= 512u)
-        append_kernel<T, 2><<<grid, 256, 0, s>>>(kv, batch, rows);
-    else if (vectors <= 1024u)
-        append_kernel<T, 4><<<grid, 256, 0, s>>>(kv, batch, rows);
-    else
-        append_kernel<T, 8><<<grid, 256, 0, s>>>(kv, batch, rows);
+    const uint32_t sides = 2u * kv.heads;
+    if (!batch.row_start) {
+        const uint64_t warps = (uint64_t)batch.n * sides;
+        return launch_dependent(append_one_kernel<T>, dim3((unsigned)((warps + 7u) / 8u)), 256u, s, kv, batch, rows);
+    }
+    const uint32_t items = item_of(batch.rows, batch.n, kv.page_shift), vectors = kv.page() * kv.dim / 8u;
+    // eight heads in a row hide the search and the first loads; with few pages the heads are spread over more blocks
+    const uint32_t per_block = items >= 256u ? 8u : 2u;
+    const dim3 grid(items, (sides + per_block - 1u) / per_block);
+    return vectors <= 256u    ? launch_dependent(append_kernel<T, 1>, grid, 256u, s, kv, batch, rows, per_block)
+           : vectors <= 512u  ? launch_dependent(append_kernel<T, 2>, grid, 256u, s, kv, batch, rows, per_block)
+           : vectors <= 1024u ? launch_dependent(append_kernel<T, 4>, grid, 256u, s, kv, batch, rows, per_block)
+                              : launch_dependent(append_kernel<T, 8>, grid, 256u, s, kv, batch, rows, per_block);
 }
 
 }  // namespace
@@ -216,14 +320,10 @@ extern "C" entro_status entro_kv_append(const entro_kv_cache* cache, const entro
     if (entro_status e = kv_check(cache, b, &batch)) return e;
     if (batch.n == 0 || batch.rows == 0) return ENTRO_OK;
     if (entro_status e = check_rows(r, &rows)) return e;
-    const uint32_t items = batch.row_start ? item_of(batch.rows, batch.n, kv.page_shift) : batch.n;
-    const dim3 grid(items, kv.heads, 2);
-    if (r->type == ENTRO_FLOAT16)
-        launch_append<__half>(kv, batch, rows, grid, (cudaStream_t)cuda_stream);
-    else
-        launch_append<__nv_bfloat16>(kv, batch, rows, grid, (cudaStream_t)cuda_stream);
+    const cudaStream_t s = (cudaStream_t)cuda_stream;
+    const cudaError_t e = r->type == ENTRO_FLOAT16 ? launch_append<__half>(kv, batch, rows, s) : launch_append<__nv_bfloat16>(kv, batch, rows, s);
+    ENTRO_CUDA(e);
     count_launch();
-    ENTRO_CUDA(cudaGetLastError());
     return ENTRO_OK;
 }
 
@@ -237,11 +337,11 @@ extern "C" entro_status entro_kv_read(const entro_kv_cache* cache, const entro_k
     if (entro_status e = kv_check(cache, b, &batch)) return e;
     if (batch.n == 0 || batch.rows == 0) return ENTRO_OK;
     if (entro_status e = check_rows(r, &rows)) return e;
-    if (r->type == ENTRO_FLOAT16)
-        read_kernel<__half><<<batch.rows, 256, 0, (cudaStream_t)cuda_stream>>>(kv, batch, rows);
-    else
-        read_kernel<__nv_bfloat16><<<batch.rows, 256, 0, (cudaStream_t)cuda_stream>>>(kv, batch, rows);
+    const dim3 grid((batch.rows + 7u) / 8u);
+    const cudaStream_t s = (cudaStream_t)cuda_stream;
+    const cudaError_t e = r->type == ENTRO_FLOAT16 ? launch_dependent(read_kernel<__half>, grid, 256u, s, kv, batch, rows)
+                                                   : launch_dependent(read_kernel<__nv_bfloat16>, grid, 256u, s, kv, batch, rows);
+    ENTRO_CUDA(e);
     count_launch();
-    ENTRO_CUDA(cudaGetLastError());
     return ENTRO_OK;
 }

@@ -180,6 +180,7 @@ template <typename T, int kDim, int kTiles>
 __global__ void __launch_bounds__(kTokenThreads, kTiles == 1 ? 2 : 1)
     token_attention_kernel(Kv kv, KvBatch batch, Query q, float* partials, uint32_t most_rows)
 {
+    dependent_start();
     constexpr uint32_t kCols = 8 * kTiles;
     constexpr int kSteps = kDim / 16;            // products of a slice's first matrix product; words of a key row
     constexpr int kWords = kDim / 32;            // words of a value row
@@ -611,8 +612,7 @@ cudaError_t launch_tokens(const Kv& kv, const KvBatch& batch, const Query& q, ui
     const uint32_t smem = kTokenWarps * kTokenStageBytes<kDim> * (one ? kTokenStages<kDim, 1> : kTokenStages<kDim, 2>);
     static std::atomic<uint64_t> allowed[2];         // bit per device: the kernel may use that much shared memory there
     if (cudaError_t e = allow_shared((const void*)kernel, smem, allowed[one])) return e;
-    kernel<<<(one ? 2u : 1u) * sm_count, kTokenThreads, smem, s>>>(kv, batch, q, partials, most_rows);
-    return cudaGetLastError();
+    return launch_dependent_shared(kernel, dim3((one ? 2u : 1u) * sm_count), kTokenThreads, smem, s, kv, batch, q, partials, most_rows);
 }
 
 }  // namespace
