@@ -1,0 +1,158 @@
+"""Token generation from entropy-coded weights and an 8-bit key/value cache, small and complete.
+
+The memory that a generation step reads is the weights and the cache; here both are in 8 bits or
+fewer and stay so: the projections are fused decode + matrix-vector products on the compressed
+streams (entro_gemv_prepare / entro_gemv_run), keys and values go into a paged cache
+(entro_kv_reserve, entro_kv_append) and are attended to where they lie (entro_kv_attention), and the
+sequences of a beam share the pages of their prompt (entro_kv_fork).  The prompt takes the weights
+decoded once (entro_decode_dequant) and the attention's prompt form.  Weights are seeded synthetic
+tensors, so the tokens mean nothing; what it shows is the calls in their order.
+
+    python -m paper_2505_02380_b200.generate [--layers 2] [--prompt 300] [--tokens 32] [--beams 4]
+"""
+from __future__ import annotations
+
+import argparse
+import json
+from typing import List, Optional
+
+import torch
+
+import paper_2505_02380_b200 as E
+import workloads
+
+
+class Projection:
+    """One compressed weight matrix, decoded inside a product with up to `batch` tokens."""
+
+    def __init__(self, rows: int, cols: int, batch: int, seed: int, bits: int = 8, chunk: int = 4096):
+        w = workloads.make_values(rows * cols, 0.7 * cols ** -0.5, seed, device="cuda")
+        q, qp = E.entro_quantize_tensor(w, bits)
+        counts = E.entro_histogram(q, bits).tolist()
+        self.cb = E.entro_build_codebook(counts)
+        self.enc = E.entro_encode(q, self.cb, chunk, stream_words=E.entro_stream_words(counts, self.cb))
+        self.shape, self.qp = (rows, cols), qp
+        self.x = torch.zeros(batch, cols, dtype=torch.float16, device="cuda")
+        desc = E.make_desc_no_out(self.enc.stream, self.enc.index, rows * cols, chunk, self.cb, qp.scale, qp.zero_point)
+        self.plan, (self.y,) = E.entro_gemv_prepare([desc], [self.x], [self.shape])
+
+    def decoded(self) -> torch.Tensor:
+        return E.entro_decode_dequant(self.enc.stream, self.enc.index, self.shape[0] * self.shape[1], self.enc.chunk_symbols,
+                                      self.cb, self.qp.scale, self.qp.zero_point).view(self.shape)
+
+    def step(self, x: torch.Tensor) -> torch.Tensor:
+        """One token of each sequence: x [batch, cols] -> [batch, rows], the weights read as they are stored."""
+        self.x.copy_(x)
+        E.entro_gemv_run(self.plan)
+        return self.y
+
+
+def _norm(x: torch.Tensor) -> torch.Tensor:
+    return (x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-5)).half()
+
+
+def _rotate(x: torch.Tensor, position: torch.Tensor) -> torch.Tensor:
+    """Rotary position embedding of [rows, heads, dim]."""
+    half = x.shape[-1] // 2
+    angle = position[:, None, None].float() * (10000.0 ** (-torch.arange(half, device=x.device).float() / half))
+    a, b = x[..., :half].float(), x[..., half:].float()
+    return torch.cat([a * angle.cos() - b * angle.sin(), a * angle.sin() + b * angle.cos()], -1).half()
+
+
+class Layer:
+    def __init__(self, model: "Model", seed: int):
+        h, q, kv = model.hidden, model.heads * model.dim, model.kv_heads * model.dim
+        self.qkv = Projection(q + 2 * kv, h, model.beams, seed)
+        self.out = Projection(h, q, model.beams, seed + 1)
+        self.up = Projection(2 * model.hidden, h, model.beams, seed + 2)
+        self.down = Projection(h, 2 * model.hidden, model.beams, seed + 3)
+        self.kv: Optional[E.KvCache] = None
+
+
+class Model:
+    """A decoder with rotary positions, grouped heads, a sliding window with sinks, and a paged cache per layer."""
+
+    def __init__(self, layers: int = 2, hidden: int = 512, heads: int = 8, kv_heads: int = 2, dim: int = 64, vocabulary: int = 1024,
+                 page: int = 16, max_tokens: int = 1024, beams: int = 4, window: int = 256, sinks: int = 4, seed: int = 1):
+        self.hidden, self.heads, self.kv_heads, self.dim, self.beams = hidden, heads, kv_heads, dim, beams
+        self.window, self.sinks = window, sinks
+        self.layers: List[Layer] = [Layer(self, seed + 10 * i) for i in range(layers)]
+        self.head = Projection(vocabulary, hidden, beams, seed + 1000)
+        self.embedding = workloads.make_values(vocabulary * hidden, 1.0, seed + 1001, device="cuda").view(vocabulary, hidden)
+        pages = (max_tokens + page - 1) // page + beams * (max_tokens // 4 // page + 2)
+        for layer in self.layers:       # one work area: the layers' calls follow one another on one stream
+            layer.kv = E.entro_kv_create(pages, kv_heads, dim, page, beams, max_tokens,
+                                         work=None if layer is self.layers[0] else self.layers[0].kv.work)
+
+    def _attend(self, layer: Layer, qkv: torch.Tensor, position: torch.Tensor, slots: torch.Tensor,
+                row_start: Optional[torch.Tensor], max_rows: int) -> torch.Tensor:
+        q, k, v = qkv.view(-1, self.heads + 2 * self.kv_heads, self.dim).split([self.heads, self.kv_heads, self.kv_heads], 1)
+        q, k = _rotate(q, position), _rotate(k, position)
+        rows = qkv.shape[0]
+        E.entro_kv_reserve(layer.kv, rows, slots=slots, row_start=row_start)
+        E.entro_kv_append(layer.kv, k, v, slots=slots, row_start=row_start)
+        out = E.entro_kv_attention(layer.kv, q, slots=slots, row_start=row_start, max_rows=max_rows, window=self.window, sinks=self.sinks)
+        E.entro_kv_trim(layer.kv, slots, self.window, self.sinks)        # pages that no later token sees
+        return out.view(rows, -1)
+
+    def _run(self, x: torch.Tensor, position, slots, row_start, max_rows, step: bool) -> torch.Tensor:
+        apply = (lambda p, a: p.step(a)) if step else (lambda p, a: torch.matmul(a, p.decoded().t()))
+        for layer in self.layers:
+            x = x + apply(layer.out, self._attend(layer, apply(layer.qkv, _norm(x)), position, slots, row_start, max_rows))
+            x = x + apply(layer.down, torch.nn.functional.silu(apply(layer.up, _norm(x))))
+        return apply(self.head, _norm(x)).float()
+
+    def prompt(self, tokens: torch.Tensor, slot: int = 0) -> torch.Tensor:
+        """-> logits of all its tokens [tokens, vocabulary]; the sequence lies in `slot` afterwards."""
+        n = tokens.shape[0]
+        slots = torch.tensor([slot], dtype=torch.int32, device="cuda")
+        starts = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+        return self._run(self.embedding[tokens], torch.arange(n, device="cuda"), slots, starts, n, False)
+
+    def step(self, tokens: torch.Tensor, position: int) -> torch.Tensor:
+        """One token of every beam -> logits [beams, vocabulary]."""
+        slots = torch.arange(self.beams, dtype=torch.int32, device="cuda")
+        at = torch.full((self.beams,), position, device="cuda")
+        return self._run(self.embedding[tokens], at, slots, None, 1, True)
+
+    def fork(self, src: torch.Tensor, dst: torch.Tensor) -> None:
+        for layer in self.layers:
+            E.entro_kv_fork(layer.kv, src, dst)
+
+    def status(self) -> int:
+        return max(E.entro_kv_status(layer.kv) for layer in self.layers)
+
+
+def beam_search(model: Model, prompt: torch.Tensor, tokens: int):
+    """-> (tokens [beams, tokens], log probabilities [beams]) of the most likely continuations."""
+    logp = torch.log_softmax(model.prompt(prompt)[-1], -1)
+    every = torch.arange(model.beams, dtype=torch.int32, device="cuda")
+    model.fork(torch.zeros_like(every), every)               # all beams share the prompt's pages
+    score, last = logp.topk(model.beams)
+    out = last[:, None]
+    for i in range(tokens - 1):
+        logp = torch.log_softmax(model.step(last, prompt.shape[0] + i), -1)
+        score, best = (score[:, None] + logp).reshape(-1).topk(model.beams)
+        parent, last = best // logp.shape[1], best % logp.shape[1]
+        model.fork(parent.to(torch.int32), every)            # a beam that goes on twice shares its full pages
+        out = torch.cat([out[parent], last[:, None]], 1)
+    return out, score
+
+
+def main() -> None:
+    ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
+    ap.add_argument("--layers", type=int, default=2)
+    ap.add_argument("--prompt", type=int, default=300)
+    ap.add_argument("--tokens", type=int, default=32)
+    ap.add_argument("--beams", type=int, default=4)
+    a = ap.parse_args()
+    model = Model(layers=a.layers, beams=a.beams, max_tokens=a.prompt + a.tokens + 16)
+    prompt = torch.randint(0, 1024, (a.prompt,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(7))
+    out, score = beam_search(model, prompt, a.tokens)
+    kv = model.layers[0].kv
+    print(json.dumps({"tokens": out[0].tolist(), "log_probability": round(float(score[0]), 4),
+                      "pages_in_use": int((kv.refs > 0).sum()), "status": E.status_string(model.status())}))
+
+
+if __name__ == "__main__":
+    main()

@@ -1,0 +1,47 @@
+"""The generation example: the cached steps against the prompt form on the same tokens, and its pages."""
+import pytest
+import torch
+
+import paper_2505_02380_b200 as E
+from paper_2505_02380_b200 import generate
+
+pytestmark = pytest.mark.gpu
+
+
+def _model(**kw):
+    return generate.Model(**{**dict(layers=2, max_tokens=200, window=64, sinks=4, beams=2), **kw})
+
+
+def test_steps_give_the_logits_of_the_prompt_form():
+    """Token by token through the cache, or all at once: the same sums in another order, over the same codes but
+    for pages whose scale grows token by token (half a step of an 8-bit code, twice).  Beams need not agree bit for bit:
+    the matrix-vector products add rows that span chunks in no fixed order (entro.h, entro_decode_dequant_gemv)."""
+    tokens = torch.randint(0, 1024, (90,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    whole = _model().prompt(tokens)
+    model = _model()
+    model.prompt(tokens[:50])
+    every = torch.arange(2, dtype=torch.int32, device="cuda")
+    model.fork(torch.zeros_like(every), every)
+    steps = torch.stack([model.step(tokens[50 + i].expand(2), 50 + i).clone() for i in range(40)], 1)
+    assert model.status() == E.OK
+    for beam in steps:
+        off = (beam - whole[50:]).norm() / whole[50:].norm()
+        assert off < 0.05, off
+
+
+def test_beams_share_the_prompt_and_release_what_they_drop():
+    model = _model(beams=4)
+    prompt = torch.randint(0, 1024, (100,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(4))
+    out, score = generate.beam_search(model, prompt, 24)
+    assert out.shape == (4, 24) and (score[:-1] >= score[1:]).all()
+    assert model.status() == E.OK
+    for layer in model.layers:
+        kv = layer.kv
+        held = kv.table[kv.table >= 0].long()
+        assert torch.equal(torch.bincount(held, minlength=kv.pages).int(), kv.refs)
+        assert int((kv.refs > 0).sum()) <= 4 * 6 + 1         # window of 64 and the sinks' page, in pages of 16
+    # the best continuation scores what its tokens score one after the other
+    model = _model(beams=4)
+    logits = model.prompt(torch.cat([prompt, out[0]]))
+    logp = torch.log_softmax(logits, -1)[99:-1].gather(1, out[0][:, None]).sum()
+    assert abs(float(logp) - float(score[0])) < 0.02 * abs(float(score[0]))
