@@ -887,6 +887,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                         if (ok) {
                             tc_fence_after();
                             scores(half, (kQ >> 4 | 1u << 16) + tile * (kTile >> 4), k_low);
+                            // a tile is free as soon as its last product is done, whatever the turn still waits for
+                            if (j + 1u == pieces) commit(&sh.q_empty[tile]);
+                            if (half == 1u || !two) commit(&sh.k_empty[stage]);
                         }
                     }
                 }
@@ -897,11 +900,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 }
                 had = there;
                 if (!there) break;
-                commit(&sh.k_empty[stage]);
-                if (j + 1u == pieces) {
-                    commit(&sh.q_empty[tile0 % 3u]);
-                    if (two) commit(&sh.q_empty[(tile0 + 1u) % 3u]);
-                }
                 had_two = two;
                 had_add = j > 0u;
                 ++count;
@@ -946,6 +944,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 const uint32_t token0 = r0 / q.group, head0 = r0 - token0 * q.group;
                 const unsigned char* from = q.q + (int64_t)(unit.row0 + (int)token0) * q.q_row + (int64_t)(unit.head * q.group) * q.q_head;
                 // all of the tile's copies in flight at once
+#pragma unroll 4
                 for (uint32_t row = loader * kPerWarp + sub; row < 128u; row += 3u * kPerWarp) {
                     const uint32_t r = r0 + row, token = q.by_group(head0 + row), h = head0 + row - token * q.group;
                     unsigned char* to = tile + row * 128u + ((unit16 & 7u) ^ (row & 7u)) * 16u;
@@ -961,7 +960,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                 __syncwarp();
                 if constexpr (!__is_same(T, __half)) {
                     // bf16 to fp16 in place, a power of two taken out of each row
-#pragma unroll 4
+#pragma unroll 8
                     for (uint32_t base = loader * kPerWarp; base < 128u; base += 3u * kPerWarp) {
                         const uint32_t row = base + sub;
                         unsigned char* to = tile + row * 128u + ((unit16 & 7u) ^ (row & 7u)) * 16u;
