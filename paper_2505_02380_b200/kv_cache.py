@@ -31,6 +31,7 @@ class KvCache:
     table  int32   [slots, table_width], -1 for no page;  lens int32 [slots];  refs int32 [pages]
     work:  uint8 device memory of entro_kv_work_bytes, zero; allocated here unless another cache's
     (KvCache.work) is given, which is allowed where the two caches' calls do not overlap on the GPU.
+    One thread at a time may make calls on a handle: they pack their arguments into memory that it keeps.
     """
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
