@@ -162,9 +162,10 @@ __global__ void __launch_bounds__(256) append_one_kernel(Kv kv, KvBatch batch, R
 
 // Any number of new rows: a block per touched page and `per_block` of its heads (keys and values apart).  Bound by memory:
 // a new value is read once (2 bytes) and written once (1 byte); it waits in registers for the page's maximum, while the
-// next head's values are on their way.
+// next head's values are on their way.  Five blocks an SM where the registers allow it: 148 us
+// instead of 153 for prompts of 700 .. 4096 rows written and read back.
 template <typename T, int kVec>
-__global__ void __launch_bounds__(256) append_kernel(Kv kv, KvBatch batch, Rows rows, uint32_t per_block)
+__global__ void __launch_bounds__(256, kVec <= 2 ? 5 : 1) append_kernel(Kv kv, KvBatch batch, Rows rows, uint32_t per_block)
 {
     dependent_start();
     const Item it = find_item(kv, batch, blockIdx.x);
