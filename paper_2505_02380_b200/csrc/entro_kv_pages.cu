@@ -97,10 +97,45 @@ __device__ __forceinline__ void part_sums(const uint32_t* part, uint32_t* before
     }
 }
 
+// With one block (at most kPlanOne pages) the counts are read once: bit p of live[] says that page p is in use.
+constexpr uint32_t kLiveWords = kPlanOne / 32u;
+static_assert(kLiveWords <= kPlanThreads, "a thread takes a word of 32 pages");
+
+__device__ __forceinline__ void read_live(const Kv& kv, uint32_t* live)
+{
+    for (uint32_t base = 0; base < kv.pages; base += kPlanThreads) {
+        const uint32_t p = base + threadIdx.x;
+        const uint32_t bits = __ballot_sync(0xffffffffu, p < kv.pages && __ldcg(kv.refs + p) > 0);
+        if ((threadIdx.x & 31u) == 0 && p < kv.pages) live[p / 32u] = bits;
+    }
+    __syncthreads();
+}
+
+// This thread's word, and which of its pages exist.
+__device__ __forceinline__ uint32_t live_word(const Kv& kv, const uint32_t* live, uint32_t* exist)
+{
+    const uint32_t first = threadIdx.x * 32u;
+    *exist = first >= kv.pages ? 0u : kv.pages - first >= 32u ? 0xffffffffu : (1u << (kv.pages - first)) - 1u;
+    return *exist ? live[threadIdx.x] : 0u;
+}
+
 // The `want` lowest free pages in ascending order into fresh[]; returns how many there are.  The
 // caller has a barrier before (counts final) and one after (fresh[] and refs in place).
 __device__ __forceinline__ uint32_t take_lowest_free(const Kv& kv, uint32_t want, int32_t* fresh, uint32_t* part)
 {
+    if (gridDim.x == 1u) {
+        __shared__ uint32_t live[kLiveWords];
+        uint32_t exist, total;
+        read_live(kv, live);
+        uint32_t free_bits = ~live_word(kv, live, &exist) & exist;
+        uint32_t rank = block_scan(__popc(free_bits), &total);
+        for (; free_bits && rank < want; ++rank, free_bits &= free_bits - 1u) {
+            const uint32_t p = threadIdx.x * 32u + __ffs(free_bits) - 1u;
+            fresh[rank] = (int32_t)p;
+            kv.refs[p] = 1;
+        }
+        return min(total, want);
+    }
     uint32_t lo, hi, before, all;
     segment(kv.pages, &lo, &hi);
     auto is_free = [&](uint32_t p) { return __ldcg(kv.refs + p) <= 0; };
@@ -294,27 +329,45 @@ __global__ void __launch_bounds__(kPlanThreads) compact_kernel(Kv kv)
     int32_t* from = (int32_t*)kv.region;      // [pages] pages that move, ascending
     int32_t* to = from + kv.pages;            // [pages] free places that they go to, ascending
     int32_t* moved = to + kv.pages;           // [pages] new place of a page
-    uint32_t lo, hi, before, live, holes_before, holes, movers_before, movers;
-    segment(kv.pages, &lo, &hi);
-    auto is_live = [&](uint32_t p) { return __ldcg(kv.refs + p) > 0; };
-    const uint32_t mine = count_pages(lo, hi, is_live);
-    uint32_t* part = kv.head->part;
-    if (threadIdx.x == 0) part[blockIdx.x] = mine;
-    plan_barrier();
-    part_sums(part, &before, &live);
-    const uint32_t low_hi = min(hi, max(lo, live)), high_lo = max(lo, min(hi, live));
-    const uint32_t free_low = (low_hi - lo) - count_pages(lo, low_hi, is_live);
-    const uint32_t live_high = count_pages(high_lo, hi, is_live);
-    if (threadIdx.x == 0) {
-        part[kPlanMost + blockIdx.x] = free_low;
-        part[2 * kPlanMost + blockIdx.x] = live_high;
+    uint32_t live, movers;
+    if (gridDim.x == 1u) {
+        __shared__ uint32_t in_use[kLiveWords];
+        uint32_t exist, total;
+        read_live(kv, in_use);
+        const uint32_t word = live_word(kv, in_use, &exist), first = threadIdx.x * 32u;
+        block_scan(__popc(word), &live);
+        // the word's pages among the first `live` places
+        const uint32_t low = first >= live ? 0u : live - first >= 32u ? 0xffffffffu : (1u << (live - first)) - 1u;
+        uint32_t hole_bits = ~word & exist & low, mover_bits = word & ~low;
+        const uint32_t ranks = block_scan(__popc(hole_bits) | __popc(mover_bits) << 16, &total);     // two sums of at most 2^14
+        uint32_t rank = ranks & 0xffffu;
+        for (; hole_bits; ++rank, hole_bits &= hole_bits - 1u) to[rank] = (int32_t)(first + __ffs(hole_bits) - 1u);
+        rank = ranks >> 16;
+        for (; mover_bits; ++rank, mover_bits &= mover_bits - 1u) from[rank] = (int32_t)(first + __ffs(mover_bits) - 1u);
+        movers = total >> 16;
+    } else {
+        uint32_t lo, hi, before, holes_before, holes, movers_before;
+        segment(kv.pages, &lo, &hi);
+        auto is_live = [&](uint32_t p) { return __ldcg(kv.refs + p) > 0; };
+        const uint32_t mine = count_pages(lo, hi, is_live);
+        uint32_t* part = kv.head->part;
+        if (threadIdx.x == 0) part[blockIdx.x] = mine;
+        plan_barrier();
+        part_sums(part, &before, &live);
+        const uint32_t low_hi = min(hi, max(lo, live)), high_lo = max(lo, min(hi, live));
+        const uint32_t free_low = (low_hi - lo) - count_pages(lo, low_hi, is_live);
+        const uint32_t live_high = count_pages(high_lo, hi, is_live);
+        if (threadIdx.x == 0) {
+            part[kPlanMost + blockIdx.x] = free_low;
+            part[2 * kPlanMost + blockIdx.x] = live_high;
+        }
+        plan_barrier();
+        part_sums(part + kPlanMost, &holes_before, &holes);
+        part_sums(part + 2 * kPlanMost, &movers_before, &movers);
+        rank_pages(lo, low_hi, holes_before, holes, [&](uint32_t p) { return !is_live(p); },
+                   [&](uint32_t rank, uint32_t p) { to[rank] = (int32_t)p; });
+        rank_pages(high_lo, hi, movers_before, movers, is_live, [&](uint32_t rank, uint32_t p) { from[rank] = (int32_t)p; });
     }
-    plan_barrier();
-    part_sums(part + kPlanMost, &holes_before, &holes);
-    part_sums(part + 2 * kPlanMost, &movers_before, &movers);
-    rank_pages(lo, low_hi, holes_before, holes, [&](uint32_t p) { return !is_live(p); },
-               [&](uint32_t rank, uint32_t p) { to[rank] = (int32_t)p; });
-    rank_pages(high_lo, hi, movers_before, movers, is_live, [&](uint32_t rank, uint32_t p) { from[rank] = (int32_t)p; });
     plan_barrier();
     for (uint32_t k = plan_rank(); k < movers; k += gridDim.x * kPlanThreads) {
         const int f = __ldcg(from + k), t = __ldcg(to + k);
